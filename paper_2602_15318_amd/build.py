@@ -1,6 +1,8 @@
-"""Build the HIP library (gfx950) and the binding's native part in-tree: paper_2602_15318_amd/libsparrow.so, _native.so."""
+"""Build the HIP libraries (gfx950) and the binding's native part in-tree: paper_2602_15318_amd/libsparrow.so,
+libsparrow_paged.so, _native.so."""
 from __future__ import annotations
 
+import concurrent.futures
 import glob
 import importlib.util
 import os
@@ -11,6 +13,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparrow.so")
+PAGED = os.path.join(HERE, "libsparrow_paged.so")
 NATIVE = os.path.join(HERE, "_native.so")
 
 # The preload count puts the leading scalar arguments of a kernel into scalar registers at launch: a
@@ -36,10 +39,16 @@ def _run(cmd, verbose: bool) -> None:
 
 
 def build(verbose: bool = False, extra=()) -> str:
-    """Compile every csrc/*.hip into one shared library, and csrc/binding.cpp.  Always recompiles."""
-    srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
+    """Compile every csrc/*.hip into one shared library, csrc/paged/*.hip into another, and csrc/binding.cpp.  Always recompiles."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    _run([hipcc, *HIPCC_FLAGS, *extra, "-o", LIB, *srcs], verbose)
+
+    def hip(lib, *under):
+        srcs = sorted(glob.glob(os.path.join(CSRC, *under, "*.hip")))
+        _run([hipcc, *HIPCC_FLAGS, *extra, "-o", lib, *srcs], verbose)
+
+    with concurrent.futures.ThreadPoolExecutor(2) as pool:     # side by side: each is one compiler, file after file
+        for done in [pool.submit(hip, LIB), pool.submit(hip, PAGED, "paged")]:
+            done.result()
     torch = os.path.dirname(importlib.util.find_spec("torch").origin)
     _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
           "-isystem", os.path.join(torch, "include"), "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),

@@ -1,0 +1,52 @@
+// Internal interface of the paged-cache kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../../include/sparrow_paged.h"
+#include "../common.hpp"
+
+namespace sparrow {
+
+struct PageUpdateArgs {
+  const int32_t *old_len, *new_len, *pos_offset;
+  int32_t *block_table, *free_pages, *n_free, *slots, *positions, *cu_new, *status;
+  int64_t table_stride;
+  int32_t B, page_shift, table_width, capacity, n_rows;
+};
+hipError_t launch_page_update(const PageUpdateArgs &a, hipStream_t st);
+
+// Frequencies in quarter turns per position and the axis of each, by value with the launch.
+struct Frequencies {
+  double quarter[64];
+  uint8_t axis[64];
+};
+struct RopeTableArgs {
+  const int32_t *positions;
+  int64_t axis_stride;
+  float *cos, *sin;
+  int32_t N;
+};
+hipError_t launch_mrope_table(const RopeTableArgs &a, const Frequencies &f, int d, hipStream_t st);
+
+struct AppendArgs {
+  const void *q, *k, *v;
+  const int32_t *positions, *slots;
+  void *q_out, *k_cache, *v_cache;
+  int64_t axis_stride, q_row, kv_row, stride_page, stride_token, stride_head;   // elements
+  int32_t N, Hq, Hkv, page_shift, n_slots;
+};
+hipError_t launch_mrope_append(int dtype, const AppendArgs &a, const Frequencies &f, int d, hipStream_t st);
+
+struct ChunkArgs {
+  const void *q, *k, *v;
+  const int32_t *block_table, *cu_new, *kv_len;
+  void *out;
+  float *lse;
+  int64_t table_stride, q_row, stride_page, stride_token, stride_head;          // elements
+  int32_t B, n_rows, max_new, Hq, Hkv, g, table_width, page_shift, n_pages;
+  float scale_log2;
+};
+hipError_t launch_chunk_attn(int dtype, int d, const ChunkArgs &a, hipStream_t st);
+
+}  // namespace sparrow
