@@ -1,4 +1,6 @@
 // Attention of new tokens over the paged cache, plain version: a wavefront takes one (row, query head), 64 keys a round.
+#include <algorithm>
+
 #include "paged.hpp"
 
 namespace sparrow {
@@ -16,8 +18,8 @@ __global__ void __launch_bounds__(256) chunk_attn_plain_kernel(ChunkArgs a) {
   for (int k = 0; k < a.B; ++k)
     if (r >= a.cu_new[k] && r < a.cu_new[k + 1]) { b = k; break; }
   if (b < 0 || r - a.cu_new[b] >= a.max_new) return;
-  const int L = min(max(a.kv_len[b], 0), a.table_width << a.page_shift);
-  const int pos = min(L - 1, a.kv_len[b] - (a.cu_new[b + 1] - a.cu_new[b]) + (r - a.cu_new[b]));
+  const int kv = max(a.kv_len[b], 0), L = min(kv, a.table_width << a.page_shift);
+  const int pos = min(L - 1, kv - (min(a.cu_new[b + 1], a.n_rows) - a.cu_new[b]) + (r - a.cu_new[b]));
   const int32_t *table = a.block_table + b * a.table_stride;
   auto row_of = [&](int t) {
     const unsigned page = min((unsigned)table[t >> a.page_shift], (unsigned)(a.n_pages - 1));
@@ -62,7 +64,28 @@ __global__ void __launch_bounds__(256) chunk_attn_plain_kernel(ChunkArgs a) {
 
 }  // namespace
 
+hipError_t launch_chunk_few(int d, int rows, const ChunkArgs &a, hipStream_t st);
+hipError_t launch_chunk_combine(int dtype, int d, int rows, const ChunkArgs &a, hipStream_t st);
+
+ChunkShape chunk_shape(int dtype, int d, int Hq, int Hkv, int B, int64_t n_rows, int max_new) {
+  ChunkShape s{0, 0, 0, 0};
+  const int64_t rows = std::min<int64_t>(max_new, n_rows) * (Hq / Hkv);
+  if (dtype == SPARROW_BF16 && rows <= 64) {
+    s.rows = rows <= 32 ? 32 : 64;
+    s.slots = std::max(256 / Hkv, 2 * B);
+    const int64_t units = (int64_t)s.slots * Hkv * s.rows;
+    s.floats_o = units * d;
+    s.floats_ml = units * 2;
+  }
+  return s;
+}
+
 hipError_t launch_chunk_attn(int dtype, int d, const ChunkArgs &a, hipStream_t st) {
+  const ChunkShape s = chunk_shape(dtype, d, a.Hq, a.Hkv, a.B, a.n_rows, a.max_new);
+  if (s.rows > 0) {
+    if (const hipError_t e = launch_chunk_few(d, s.rows, a, st); e != hipSuccess) return e;
+    return launch_chunk_combine(dtype, d, s.rows, a, st);
+  }
   const dim3 grid((unsigned)(((int64_t)a.n_rows * a.Hq + 3) / 4)), block(256);
   if (dtype == SPARROW_BF16) {
     if (d == 128) hipLaunchKernelGGL((chunk_attn_plain_kernel<bf16_t, 128>), grid, block, 0, st, a);

@@ -1,0 +1,124 @@
+// Building blocks of the chunk attention on the matrix cores, bf16: tiles of pages in LDS, operands, softmax of a tile.
+//
+// With v_mfma_f32_32x32x16_bf16 (A: 32 x 16, lane = row + 32 * (k / 8), eight k each; B: 16 x 32, lane = column + 32 * (k / 8); D: 32 x
+// 32, lane = column + 32 * h, element e in row 8 (e / 4) + 4 h + e % 4):
+//   S^T = K Q^T    a lane holds, for its row of the batch (column lane % 32), the scores of keys 8 (e / 4) + 4 h + e % 4 of 32.
+//   O^T += V^T P^T  the k index of a 16-key step is taken in the order in which the lanes hold the scores, so P^T is the scores' own
+//                 registers and V^T two transposing reads (ds_read_b64_tr_b16) of four keys each.
+#pragma once
+#include "chunk_plan.hpp"
+
+namespace sparrow {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+constexpr float kSlack = 8.0f;            // log2 units a score may exceed a row's reference point
+
+// 16 bytes per lane from base + off to LDS, lane l's at dst + 16 l (base and dst uniform).  Not counted by the compiler: wait_loads()
+// waits.  The wait states are those between a scalar register written by the vector ALU, or M0, and its use here.
+template <bool kNt> __device__ __forceinline__ void global_to_lds(const void *base, unsigned int off, unsigned int dst) {
+  if constexpr (kNt)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(dst), "v"(off), "s"(base) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void global_to_lds_each(const void *at, unsigned int dst) {      // an address of its own per lane
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(at) : "memory", "m0");
+}
+
+// Rows of a tile: 2 kD bytes, the 16-byte chunks XOR-swizzled by the row so that eight consecutive rows read at one chunk, and four rows
+// read transposed, fall on different banks.  What loads a tile writes LDS in lane order, so the lane picks the chunk that belongs there.
+template <int kD> struct Tile {
+  static constexpr int kRow = 2 * kD, kChunks = kD / 8, kLoadRows = 64 / kChunks;    // rows that one load of a wavefront covers
+  static __device__ __forceinline__ int swz(int row) { return kD == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; }
+  static __device__ __forceinline__ int at(int row, int chunk) { return row * kRow + ((chunk ^ swz(row)) << 4); }
+  // Chunk that lane `lane` of load number j (of consecutive kLoadRows rows) fetches
+  static __device__ __forceinline__ int chunk(int lane, int j) { return (lane % kChunks) ^ swz(lane / kChunks + kLoadRows * (j & 1)); }
+};
+
+// The pages of a request's KV head: where the rows from a token on are.  Rows of one load lie on one page (16 tokens and more).
+struct Pages {
+  const int32_t __attribute__((address_space(4))) *table;     // read through the scalar cache
+  const unsigned char *k, *v;                                  // the head's first row
+  int64_t stride_page;                                         // bytes
+  unsigned int stride_token;
+  int shift, last;                                             // last page entry that the request holds
+  unsigned int last_page;
+  __device__ __forceinline__ int64_t offset(int t) const {     // t uniform; tokens past the request: some row of its last page
+    const unsigned int page = min((unsigned int)table[min(t >> shift, last)], last_page);
+    return (int64_t)page * stride_page + (int64_t)(t & ((1 << shift) - 1)) * stride_token;
+  }
+};
+__device__ __forceinline__ Pages pages_of(const ChunkArgs &a, const Piece &pc, int c) {
+  Pages p;
+  p.table = (const int32_t __attribute__((address_space(4))) *)(uintptr_t)(a.block_table + (int64_t)pc.b * a.table_stride);
+  p.k = (const unsigned char *)a.k + 2 * (int64_t)c * a.stride_head;
+  p.v = (const unsigned char *)a.v + 2 * (int64_t)c * a.stride_head;
+  p.stride_page = 2 * a.stride_page;
+  p.stride_token = (unsigned int)(2 * a.stride_token);
+  p.shift = a.page_shift;
+  p.last = max(pc.rq.L - 1, 0) >> a.page_shift;
+  p.last_page = (unsigned int)(a.n_pages - 1);
+  return p;
+}
+
+__device__ __forceinline__ bf16x8 lds_b128(const unsigned char *p) { return *reinterpret_cast<const bf16x8 *>(p); }
+__device__ __forceinline__ bf16x4 lds_tr(const unsigned char *p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)p);
+}
+// V^T operand of the 16-key step `s` and 32-wide d-block `db` of a tile.  Lane: d 32 db + lane % 32, keys 16 s + 8 jj + 4 h + 0..3.
+template <int kD> __device__ __forceinline__ bf16x8 read_vt(const unsigned char *V, int s, int db, int lane) {
+  const int p = lane & 15, h = lane >> 5, row = 16 * s + 4 * h + (p >> 2);
+  const int chunk = 4 * db + 2 * ((lane >> 4) & 1) + ((p >> 1) & 1);
+  const bf16x4 x = lds_tr(V + Tile<kD>::at(row, chunk) + 8 * (p & 1));
+  const bf16x4 y = lds_tr(V + Tile<kD>::at(row + 8, chunk) + 8 * (p & 1));
+  return (bf16x8)__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+__device__ __forceinline__ float pair_max(float v) {            // over lanes l and l ^ 32
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float pair_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Elements of an operand that are no numbers: bit masks of their halves.
+__device__ __forceinline__ unsigned int no_numbers(unsigned int w) {
+  return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
+// O^T += V^T P^T of one operand of a tile in which some rows do not see some keys.  0 * inf must not reach those rows, so what is no number
+// leaves the operand; whether a row sees one such value or more is counted by products of ones, exactly, and adds the infinities then (a NaN
+// counts as both).
+__device__ __forceinline__ f32x16 add_masked(bf16x8 v, bf16x8 p, bf16x8 seen, f32x16 o) {
+  u32x4 w = __builtin_bit_cast(u32x4, v), bad;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bad[i] = no_numbers(w[i]);
+  const bool any = (bad[0] | bad[1] | bad[2] | bad[3]) != 0u;
+  if (__builtin_amdgcn_ballot_w64(any) == 0ull) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, o, 0, 0, 0);
+  u32x4 up, down;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    unsigned int u = 0u, d = 0u;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const unsigned int x = (w[i] >> (16 * half)) & 0xffffu;
+      const bool no = (x & 0x7f80u) == 0x7f80u, nan = no && (x & 0x7fu) != 0u;
+      if (no && (nan || (x & 0x8000u) == 0u)) u |= 0x3f80u << (16 * half);      // 1.0
+      if (no && (nan || (x & 0x8000u) != 0u)) d |= 0x3f80u << (16 * half);
+    }
+    up[i] = u;
+    down[i] = d;
+    w[i] &= ~bad[i];
+  }
+  o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p, o, 0, 0, 0);
+  const f32x16 zero = {0.f};
+  const f32x16 cu = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, up), seen, zero, 0, 0, 0);
+  const f32x16 cd = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, down), seen, zero, 0, 0, 0);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) o[e] += (cu[e] > 0.f ? INFINITY : 0.f) + (cd[e] > 0.f ? -INFINITY : 0.f);
+  return o;
+}
+
+}  // namespace sparrow

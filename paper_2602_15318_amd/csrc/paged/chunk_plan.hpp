@@ -1,0 +1,133 @@
+// Which piece of the batch a workgroup of the chunk attention takes.  Lengths live on the device, so the workgroups work the
+// plan out themselves, each the same one: a wavefront holds a request per lane (and register, above 64 requests).
+//
+// A row is a (new token, query head of the group) pair; the rows of a request and KV head are cut into blocks of kBM rows, a
+// block's keys into pieces.  With N pieces to hand out per KV head and U blocks in the batch, pieces are of
+// T = sum(blocks * length) / (N - U) tokens at most: the sum over the blocks of ceil(length / T) is then at most N.  Blocks
+// are not cut at all where N is not above U.
+#pragma once
+#include "paged.hpp"
+
+namespace sparrow {
+
+template <int kCtrl, int kRows> __device__ __forceinline__ int dpp_from(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xF, false);
+}
+// Inclusive sum over the lanes of a wavefront, on the vector ALU
+__device__ __forceinline__ int wave_scan(int v) {
+  v += dpp_from<0x111, 0xF>(v);          // row_shr 1, 2, 4, 8: within each row of 16 lanes
+  v += dpp_from<0x112, 0xF>(v);
+  v += dpp_from<0x114, 0xF>(v);
+  v += dpp_from<0x118, 0xF>(v);
+  v += dpp_from<0x142, 0xA>(v);          // row_bcast 15, 31: the rows before
+  v += dpp_from<0x143, 0xC>(v);
+  return v;
+}
+__device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+
+struct Request {
+  int row0, n_all, n, L, past;     // first row; new tokens; those computed; tokens in the cache; position of the first new one
+};
+__device__ __forceinline__ Request request_of(const ChunkArgs &a, int b) {
+  Request r;
+  const int c0 = min(max(a.cu_new[b], 0), a.n_rows), c1 = min(max(a.cu_new[b + 1], 0), a.n_rows), kv = max(a.kv_len[b], 0);
+  r.row0 = c0;
+  r.n_all = max(c1 - c0, 0);
+  r.n = min(r.n_all, a.max_new);
+  r.L = min(kv, a.table_width << a.page_shift);
+  r.past = kv - r.n_all;
+  return r;
+}
+
+// floor(x / y) for 0 <= x < 2^31, y >= 1 and a quotient below 2^22
+__device__ __forceinline__ int quotient(int x, int y, float inv_y) {
+  int q = (int)((float)x * inv_y);
+  const int r = x - q * y;
+  return r < 0 ? q - 1 : r >= y ? q + 1 : q;
+}
+__device__ __forceinline__ int quotient(int x, int y) {
+  return __builtin_amdgcn_readfirstlane(quotient(x, y, __builtin_amdgcn_rcpf((float)y)));
+}
+
+struct Piece {
+  Request rq;
+  int b, block, n_blocks, split, n_splits, first, t0, t1;    // first: number of the request's first piece
+};
+constexpr int kMaxPerLane = SPARROW_MAX_PAGED_BATCH / 64;
+constexpr int kGrain = 64;                                    // pieces are whole multiples of this many tokens
+
+struct Plan {
+  int T, n_blocks[kMaxPerLane], n_splits[kMaxPerLane], end[kMaxPerLane];
+  Request rq[kMaxPerLane];
+};
+// Lane l's requests l, l + 64, ...
+template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a, int lane) {
+  Plan p;
+  int blocks = 0;
+  float weight = 0.f;
+#pragma unroll
+  for (int k = 0; k < kMaxPerLane; ++k) {
+    p.n_blocks[k] = 0;
+    p.rq[k] = {0, 0, 0, 0, 0};
+    if (64 * k < a.B) {
+      if (64 * k + lane < a.B) {
+        p.rq[k] = request_of(a, 64 * k + lane);
+        p.n_blocks[k] = (int)(((int64_t)p.rq[k].n * a.g + kBM - 1) / kBM);
+      }
+      blocks += min(p.n_blocks[k], a.slots);               // (offsets that overlap may promise any number)
+      weight += (float)p.n_blocks[k] * (float)p.rq[k].L;
+    }
+  }
+  const int U = lane_value(wave_scan(blocks), 63);
+  const float W = wave_sum_valu(weight);
+  p.T = 1 << 30;
+  // (the factor: the sum is off by 2^-16 at most)
+  if (a.slots > U) p.T = (min((int)(W * (1.f + 0x1p-14f) / (float)(a.slots - U)), 1 << 29) + kGrain) / kGrain * kGrain;
+  const float inv_T = __builtin_amdgcn_rcpf((float)p.T);
+  int before = 0;
+#pragma unroll
+  for (int k = 0; k < kMaxPerLane; ++k) {
+    p.n_splits[k] = 1;
+    p.end[k] = before;
+    if (64 * k < a.B) {
+      p.n_splits[k] = quotient(max(p.rq[k].L - 1, 0), p.T, inv_T) + 1;
+      p.end[k] = before + wave_scan(p.n_blocks[k] * p.n_splits[k]);
+      before = lane_value(p.end[k], 63);
+    }
+  }
+  return p;
+}
+
+// Piece number `idx` of a KV head; false: there are not that many.  Blocks count down: the last, whose rows see most, come first.
+template <int kBM> __device__ __forceinline__ bool find_piece(const ChunkArgs &a, int idx, int lane, Piece *out) {
+  const Plan p = make_plan<kBM>(a, lane);
+  Piece q;
+  q.b = -1;
+  int end = 0;
+#pragma unroll
+  for (int k = 0; k < kMaxPerLane; ++k)
+    if (q.b < 0 && 64 * k < a.B) {
+      const unsigned long long m = __builtin_amdgcn_ballot_w64(p.end[k] > idx);
+      if (m != 0ull) {
+        const int l = __builtin_ctzll(m);
+        q.b = 64 * k + l;
+        q.n_blocks = lane_value(p.n_blocks[k], l);
+        q.n_splits = lane_value(p.n_splits[k], l);
+        end = lane_value(p.end[k], l);
+        q.rq = {lane_value(p.rq[k].row0, l), lane_value(p.rq[k].n_all, l), lane_value(p.rq[k].n, l), lane_value(p.rq[k].L, l),
+                lane_value(p.rq[k].past, l)};
+      }
+    }
+  if (q.b < 0) return false;
+  q.first = end - q.n_blocks * q.n_splits;
+  q.split = quotient(idx - q.first, q.n_blocks);
+  q.block = q.n_blocks - 1 - (idx - q.first - q.split * q.n_blocks);
+  if (q.block < 0 || q.block >= q.n_blocks || q.split < 0 || q.split >= q.n_splits) return false;    // (sums of such offsets that wrapped)
+  const int each = (quotient(q.rq.L + q.n_splits - 1, q.n_splits) + kGrain - 1) / kGrain * kGrain;
+  q.t0 = min(q.rq.L, q.split * each);
+  q.t1 = min(q.rq.L, q.t0 + each);
+  *out = q;
+  return true;
+}
+
+}  // namespace sparrow

@@ -22,6 +22,8 @@ int fail(int code, const char *fmt, ...) {
 
 bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
 int shift_of(int32_t page_size) { return 31 - __builtin_clz((unsigned)page_size); }
 
 int check_page_size(int32_t page_size) {
@@ -179,8 +181,11 @@ int sparrow_mrope_append(const sparrow_paged_desc *desc, const void *q, const vo
 }
 
 size_t sparrow_chunk_attn_workspace(const sparrow_paged_desc *desc, int32_t B, int32_t n_rows, int32_t max_new) {
-  (void)desc; (void)B; (void)n_rows; (void)max_new;
-  return 0;
+  if (!desc || desc->n_q_heads <= 0 || desc->n_kv_heads <= 0 || desc->n_q_heads % desc->n_kv_heads != 0 || B <= 0 || n_rows <= 0 ||
+      max_new <= 0)
+    return 0;
+  const ChunkShape s = chunk_shape(desc->dtype, desc->head_dim, desc->n_q_heads, desc->n_kv_heads, B, n_rows, max_new);
+  return round_up((size_t)s.floats_o * 4, 256) + round_up((size_t)s.floats_ml * 4, 256);
 }
 
 int sparrow_chunk_attn(const sparrow_paged_desc *desc, const void *q, const void *k_cache, const void *v_cache,
@@ -214,6 +219,11 @@ int sparrow_chunk_attn(const sparrow_paged_desc *desc, const void *q, const void
   a.g = desc->n_q_heads / desc->n_kv_heads;
   a.table_width = table_width; a.page_shift = shift_of(desc->page_size); a.n_pages = desc->n_pages;
   a.scale_log2 = (desc->scale > 0.f ? desc->scale : 1.0f / std::sqrt((float)desc->head_dim)) * kLog2e;
+  a.inv_g = 1.0f / (float)a.g;
+  const ChunkShape shape = chunk_shape(desc->dtype, desc->head_dim, a.Hq, a.Hkv, B, n_rows, max_new);
+  a.slots = shape.slots;
+  a.part_o = (float *)workspace;
+  a.part_ml = (float *)((unsigned char *)workspace + round_up((size_t)shape.floats_o * 4, 256));
   const hipError_t e = launch_chunk_attn(desc->dtype, desc->head_dim, a, (hipStream_t)hip_stream);
   if (e != hipSuccess) return fail(SPARROW_ERR_DEVICE, "chunk_attn launch: %s", hipGetErrorString(e));
   return SPARROW_OK;
