@@ -119,7 +119,7 @@ int sparrow_mrope_append(const sparrow_paged_desc *desc, const void *q, const vo
  *  out          dev [n_rows, Hq, d];  lse dev float [n_rows, Hq] or NULL
  *  workspace    dev, 256-byte aligned, at least sparrow_chunk_attn_workspace() bytes; calls that may run at the same time
  *               need one each
- *  Limits: B <= SPARROW_MAX_PAGED_BATCH, table_width * page_size <= SPARROW_MAX_PAGED_TOKENS, n_rows * Hq < 2^31.
+ *  Limits: B <= SPARROW_MAX_PAGED_BATCH, table_width * page_size and n_rows <= SPARROW_MAX_PAGED_TOKENS, n_rows * Hq < 2^31.
  *  Values and keys that a row does not see do not reach it, infinities and NaN included.
  *  B = 0, n_rows = 0 or max_new = 0: nothing is enqueued.
  */

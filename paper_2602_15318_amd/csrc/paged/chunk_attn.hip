@@ -65,25 +65,38 @@ __global__ void __launch_bounds__(256) chunk_attn_plain_kernel(ChunkArgs a) {
 }  // namespace
 
 hipError_t launch_chunk_few(int d, int rows, const ChunkArgs &a, hipStream_t st);
+hipError_t launch_chunk_many(int d, int blocks, const ChunkArgs &a, hipStream_t st);
 hipError_t launch_chunk_combine(int dtype, int d, int rows, const ChunkArgs &a, hipStream_t st);
 
 ChunkShape chunk_shape(int dtype, int d, int Hq, int Hkv, int B, int64_t n_rows, int max_new) {
   ChunkShape s{0, 0, 0, 0};
   const int64_t rows = std::min<int64_t>(max_new, n_rows) * (Hq / Hkv);
-  if (dtype == SPARROW_BF16 && rows <= 64) {
+  if (dtype != SPARROW_BF16) return s;
+  if (rows <= 64) {
     s.rows = rows <= 32 ? 32 : 64;
     s.slots = std::max(256 / Hkv, 2 * B);
-    const int64_t units = (int64_t)s.slots * Hkv * s.rows;
-    s.floats_o = units * d;
-    s.floats_ml = units * 2;
+  } else {
+    s.rows = 256;
+    const int64_t blocks = (n_rows * (Hq / Hkv) + 255) / 256;
+    s.slots = blocks * Hkv <= 128 ? 256 / Hkv : 0;         // (cut only where every block gets two pieces and more)
   }
+  const int64_t units = (int64_t)s.slots * Hkv * s.rows;
+  s.floats_o = units * d;
+  s.floats_ml = units * 2;
   return s;
 }
 
 hipError_t launch_chunk_attn(int dtype, int d, const ChunkArgs &a, hipStream_t st) {
   const ChunkShape s = chunk_shape(dtype, d, a.Hq, a.Hkv, a.B, a.n_rows, a.max_new);
   if (s.rows > 0) {
-    if (const hipError_t e = launch_chunk_few(d, s.rows, a, st); e != hipSuccess) return e;
+    hipError_t e;
+    if (s.rows < 256) {
+      e = launch_chunk_few(d, s.rows, a, st);
+    } else {                                               // every request ends in a block of its own, not all of it filled
+      const int64_t blocks = std::max<int64_t>(((int64_t)a.n_rows * a.g) / 256 + a.B, s.slots);
+      e = launch_chunk_many(d, (int)blocks, a, st);
+    }
+    if (e != hipSuccess || s.slots == 0) return e;
     return launch_chunk_combine(dtype, d, s.rows, a, st);
   }
   const dim3 grid((unsigned)(((int64_t)a.n_rows * a.Hq + 3) / 4)), block(256);

@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few_kernel(ChunkArgs a) {
       for (int rt = 0; rt < kRT; ++rt) s[rt] = (f32x16){0.f};
 #pragma unroll
       for (int ks = 0; ks < kKS; ++ks) {
-        const bf16x8 k = lds_b128(K + Tile<kD>::at(lane & 31, 2 * ks + h));
+        const bf16x8 k = lds_b128(K + (k_at<kD>(lane) ^ ks << 5));
 #pragma unroll
         for (int rt = 0; rt < kRT; ++rt) s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[rt][ks], s[rt], 0, 0, 0);
       }
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few_kernel(ChunkArgs a) {
       for (int db = 0; db < kDB; ++db)
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-          const bf16x8 v = read_vt<kD>(V, st, db, lane);
+          const bf16x8 v = read_vt<kD>(V + (vt_at<kD>(lane) ^ db << 6), st);
 #pragma unroll
           for (int rt = 0; rt < kRT; ++rt)
             o[rt][db] = edge ? add_masked(v, pb[rt][st], seen[rt][st], o[rt][db])

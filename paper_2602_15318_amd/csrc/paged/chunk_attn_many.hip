@@ -1,0 +1,275 @@
+// Attention of chunks of new tokens over the paged cache, bf16: blocks of 256 rows (new token, query head of the group) per request and KV
+// head.  Bound by the matrix cores and, beside them, by the exponentials: of a tile of 64 keys a wavefront's 32 MFMAs (heads of 128)
+// take 1,024 cycles of its SIMD's matrix core, its softmax as many of the vector ALU.
+//
+// A workgroup of eight wavefronts takes one block and piece of keys; wavefront w has rows 32 w .. 32 w + 31.  Wavefronts w and w + 4 share
+// a SIMD and run half a step apart: while one is in the products of a step (scores of a tile, output of the tile before), the other is in
+// its softmax.  K and V tiles of 64 keys go memory -> LDS past the registers, four of each, asked for four half steps ahead.
+#include "chunk_attn_mfma.hpp"
+
+namespace sparrow {
+
+namespace {
+
+constexpr int kWaves = 8, kTokens = 64, kBM = 256, kStages = 4;
+
+__device__ __forceinline__ void barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int kD>
+__global__ void __launch_bounds__(64 * kWaves, 2) chunk_many_kernel(ChunkArgs a) {
+  constexpr int kDB = kD / 32, kKS = kD / 16, kHalf = kKS / 2;
+  constexpr int kTileBytes = kTokens * 2 * kD, kLoads = 8 / Tile<kD>::kLoadRows;      // of a wavefront: eight rows of a tile
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * kStages * kTileBytes];    // K tiles, V tiles
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = blockIdx.x, idx = blockIdx.y + 32768 * blockIdx.z;
+  Piece pc;
+  if (!find_piece<kBM>(a, idx, lane, &pc)) return;         // uniform
+  const Pages pages = pages_of(a, pc, c);
+  const int R = pc.rq.n * a.g, rho0 = pc.block * kBM;
+  const bool have = rho0 + 32 * w < R;                     // the wavefront has rows
+  // this lane's row, and how far the block's rows see
+  const int rho = min(rho0 + 32 * w + (lane & 31), R - 1);
+  const int i_row = quotient(rho, a.g, a.inv_g), head = c * a.g + rho - i_row * a.g;
+  const int pos = min(pc.rq.past + i_row, pc.rq.L - 1);
+  const int last_pos = min(pc.rq.past + quotient(min(rho0 + kBM, R) - 1, a.g), pc.rq.L - 1);
+  const int t1 = min(pc.t1, last_pos + 1);
+  const int n = max(t1 - pc.t0 + kTokens - 1, 0) / kTokens;
+  // tiles that all rows of the block see whole
+  const int n_full = min(n, max(min(t1, pc.rq.past + quotient(rho0, a.g) + 1) - pc.t0, 0) / kTokens);
+
+  f32x16 o[kDB];
+  float m = kNegBig, l = 0.f;
+#pragma unroll
+  for (int db = 0; db < kDB; ++db) o[db] = (f32x16){0.f};
+  if (n > 0) {
+    const unsigned int lds0 = lds_offset(lds) + 1024 * kLoads * w;
+    unsigned int off[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      off[j] = (unsigned int)(Tile<kD>::kLoadRows * j + lane / Tile<kD>::kChunks) * pages.stride_token + 16u * Tile<kD>::chunk(lane, j);
+    auto place = [&](int tile) __attribute__((always_inline)) { return pages.offset(pc.t0 + min(tile, n - 1) * kTokens + 8 * w); };
+    auto load = [&](const unsigned char *src, int64_t at, int buf) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) global_to_lds<false>(src + at, off[j], lds0 + buf * kTileBytes + 1024 * j);
+    };
+    const int64_t p0 = place(0), p1 = place(1), p2 = place(2);
+    load(pages.k, p0, 0);
+    load(pages.v, p0, kStages);
+    load(pages.k, p1, 1);
+    load(pages.v, p1, kStages + 1);
+    load(pages.k, p2, 2);
+    bf16x8 q[kKS];
+    {
+      const unsigned char *at = (const unsigned char *)a.q + 2 * ((int64_t)(pc.rq.row0 + i_row) * a.q_row + (int64_t)head * kD) + 16 * h;
+#pragma unroll
+      for (int ks = 0; ks < kKS; ++ks) q[ks] = *(const bf16x8 *)(at + 32 * ks);
+    }
+    // Half steps of tile t: A(t), its scores (and the output of tile t - 1), then B(t), its softmax; a barrier ends each.  A(t) asks for
+    // K of tile t + 3 and V of t + 2, whose places A(t - 1) was the last to read.  A wavefront ends B(t) when all but its last
+    // requests are done, those of A(t): K of t + 2 and V of t + 1 are there before either half of the workgroup begins A(t + 1).
+    int64_t at_v = p2, at_k = place(3);
+    wait_loads<0>();
+    barrier();
+    if (w >= 4) barrier();                                 // half a step behind
+    auto request = [&](int t) __attribute__((always_inline)) {
+      load(pages.k, at_k, (t + 3) & (kStages - 1));
+      load(pages.v, at_v, kStages + ((t + 2) & (kStages - 1)));
+    };
+    auto next = [&](int t) __attribute__((always_inline)) {
+      at_v = at_k;
+      at_k = place(t + 4);
+    };
+    if (!have) {
+      request(0);
+      barrier();
+      for (int t = 0; t < n; ++t) {
+        next(t);
+        wait_loads<2 * kLoads>();
+        barrier();
+        request(t + 1);
+        barrier();
+      }
+    } else {
+      f32x16 s[2];
+      bf16x8 pb[4], kf[2][kHalf];                          // kf: the first half of the columns of the next tile's K
+      auto tile = [&](int t, int stage0, int at) __attribute__((always_inline)) {
+        at += (stage0 + (t & (kStages - 1))) * kTileBytes;
+        asm volatile("" : "+v"(at));                       // (worked out here: kept, the offsets cost more registers than there are)
+        return at;
+      };
+      auto read_k = [&](int at, int ks0, bf16x8 (*k)[kHalf]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ks = 0; ks < kHalf; ++ks)
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) k[kb][ks] = lds_b128(lds + (at ^ (ks0 + ks) << 5) + 32 * kb * Tile<kD>::kRow);
+      };
+      auto multiply = [&](int ks0, bf16x8 (*k)[kHalf]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ks = 0; ks < kHalf; ++ks)
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kb][ks], q[ks0 + ks], s[kb], 0, 0, 0);
+      };
+      auto read_v = [&](int at, int db, bf16x8 *v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int st = 0; st < 4; ++st) v[st] = read_vt<kD>(lds + (at ^ db << 6), st);
+      };
+      // the scores' exponentials about the row's reference point, which moves only when a score of the wavefront's lies more than
+      // kSlack above it
+      auto softmax = [&]() __attribute__((always_inline)) {
+        float x[2][16];
+        auto shift = [&]() __attribute__((always_inline)) {
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[kb][e] = fmaf(s[kb][e], a.scale_log2, -m);
+        };
+        shift();
+        float top = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(fmaxf(top, x[0][e]), x[1][e]);
+        if (__builtin_amdgcn_ballot_w64(top > kSlack) != 0ull) {
+          float mx = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+          for (int e = 1; e < 16; ++e) mx = fmaxf(fmaxf(mx, s[0][e]), s[1][e]);
+          const float m_new = fmaxf(m, pair_max(mx * a.scale_log2)), alpha = fast_exp2(m - m_new);
+          m = m_new;
+          l *= alpha;
+#pragma unroll
+          for (int db = 0; db < kDB; ++db) o[db] *= alpha;
+          shift();
+        }
+        float sum[2] = {0.f, 0.f};
+        u32x4 pw[4];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) {
+            const float p0 = fast_exp2(x[kb][e]), p1 = fast_exp2(x[kb][e + 1]);
+            sum[0] += p0;
+            sum[1] += p1;
+            pw[2 * kb + (e >> 3)][(e & 7) >> 1] = pack_bf16x2(p0, p1);
+          }
+        l += sum[0] + sum[1];
+        asm volatile("" : "+v"(pw[0]), "+v"(pw[1]), "+v"(pw[2]), "+v"(pw[3]), "+v"(l));     // (done here, not where they are used)
+#pragma unroll
+        for (int st = 0; st < 4; ++st) pb[st] = __builtin_bit_cast(bf16x8, pw[st]);
+      };
+      const int k0 = k_at<kD>(lane), v0 = vt_at<kD>(lane);
+      auto scores = [&](int t) __attribute__((always_inline)) {       // from kf on
+        bf16x8 k2[2][kHalf];
+        read_k(tile(t, 0, k0), kHalf, k2);
+        s[0] = s[1] = (f32x16){0.f};
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(0, kf);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(kHalf, k2);
+      };
+      read_k(tile(0, 0, k0), 0, kf);
+      request(0);
+      scores(0);
+      barrier();
+      int t = 0;
+      for (; t < n_full; ++t) {
+        next(t);
+        read_k(tile(t + 1, 0, k0), 0, kf);                 // (behind the last tile: of one that nothing is done with)
+        softmax();
+        wait_loads<2 * kLoads>();
+        barrier();
+        request(t + 1);
+        const int vt = tile(t, kStages, v0);
+        bf16x8 k2[2][kHalf], v[2][4];
+        read_k(tile(t + 1, 0, k0), kHalf, k2);
+        s[0] = s[1] = (f32x16){0.f};
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(0, kf);
+        __builtin_amdgcn_sched_barrier(0);
+        read_v(vt, 0, v[0]);
+        multiply(kHalf, k2);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int db = 0; db < kDB; ++db) {
+          if (db + 1 < kDB) read_v(vt, db + 1, v[(db + 1) & 1]);
+#pragma unroll
+          for (int st = 0; st < 4; ++st) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[db & 1][st], pb[st], o[db], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        barrier();
+      }
+      for (; t < n; ++t) {                                 // tiles that some rows do not see whole: the output in the vector half step
+        next(t);
+        const int seen = min(pos, t1 - 1) - (pc.t0 + t * kTokens) - 4 * h;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[kb][e] = 32 * kb + 8 * (e >> 2) + (e & 3) <= seen ? s[kb][e] : -INFINITY;
+        softmax();
+        const int vt = tile(t, kStages, v0);
+#pragma unroll
+        for (int st = 0; st < 4; ++st) {
+          bf16x8 ones;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) ones[e] = (__bf16)(16 * st + 8 * (e >> 2) + (e & 3) <= seen ? 1.f : 0.f);
+#pragma unroll
+          for (int db = 0; db < kDB; ++db) {
+            o[db] = add_masked(read_vt<kD>(lds + (vt ^ db << 6), st), pb[st], ones, o[db]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        read_k(tile(t + 1, 0, k0), 0, kf);
+        wait_loads<2 * kLoads>();
+        barrier();
+        request(t + 1);
+        scores(t + 1);
+        barrier();
+      }
+    }
+    if (w < 4) barrier();
+    wait_loads<0>();                                       // (no load may land once the workgroup's LDS is another's)
+  }
+  // ---- the block's rows, or its partial of this piece
+  l = pair_sum(l);
+  if (rho0 + 32 * w + (lane & 31) >= R) return;
+  if (pc.n_splits == 1) {
+    const bool none = pc.rq.past + i_row < 0;
+    const int64_t to = (int64_t)(pc.rq.row0 + i_row) * a.Hq + head;
+    const float inv = none ? 0.f : 1.f / l;
+#pragma unroll
+    for (int db = 0; db < kDB; ++db)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = none ? 0.f : o[db][4 * j + e] * inv;
+        *reinterpret_cast<u32x2 *>((bf16_t *)a.out + to * kD + 32 * db + 8 * j + 4 * h) = (u32x2){pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+      }
+    if (a.lse && h == 0) a.lse[to] = none ? -INFINITY : (m + fast_log2(l)) * kLn2;
+    return;
+  }
+  if (idx >= a.slots) return;                              // (offsets that overlap)
+  const int64_t part = ((int64_t)idx * a.Hkv + c) * kBM + 32 * w + (lane & 31);
+#pragma unroll
+  for (int db = 0; db < kDB; ++db)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<f32x4 *>(a.part_o + part * kD + 32 * db + 8 * j + 4 * h) = (f32x4){o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
+  if (h == 0) {
+    a.part_ml[2 * part] = m;
+    a.part_ml[2 * part + 1] = l;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_chunk_many(int d, int blocks, const ChunkArgs &a, hipStream_t st) {
+  const dim3 grid(a.Hkv, blocks < 32768 ? blocks : 32768, (blocks + 32767) / 32768), block(64 * kWaves);
+  if (d == 128) hipLaunchKernelGGL(chunk_many_kernel<128>, grid, block, 0, st, a);
+  else hipLaunchKernelGGL(chunk_many_kernel<64>, grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace sparrow

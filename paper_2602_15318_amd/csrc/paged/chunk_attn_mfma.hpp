@@ -66,12 +66,16 @@ __device__ __forceinline__ bf16x8 lds_b128(const unsigned char *p) { return *rei
 __device__ __forceinline__ bf16x4 lds_tr(const unsigned char *p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)p);
 }
-// V^T operand of the 16-key step `s` and 32-wide d-block `db` of a tile.  Lane: d 32 db + lane % 32, keys 16 s + 8 jj + 4 h + 0..3.
-template <int kD> __device__ __forceinline__ bf16x8 read_vt(const unsigned char *V, int s, int db, int lane) {
-  const int p = lane & 15, h = lane >> 5, row = 16 * s + 4 * h + (p >> 2);
-  const int chunk = 4 * db + 2 * ((lane >> 4) & 1) + ((p >> 1) & 1);
-  const bf16x4 x = lds_tr(V + Tile<kD>::at(row, chunk) + 8 * (p & 1));
-  const bf16x4 y = lds_tr(V + Tile<kD>::at(row + 8, chunk) + 8 * (p & 1));
+// Offsets into a tile from which a lane's operands are one XOR (columns) and an immediate (rows) away: K of columns 16 ks .. by k_at ^ ks <<
+// 5, V^T of the 32-wide d-block db by vt_at ^ db << 6.
+template <int kD> __device__ __forceinline__ int k_at(int lane) { return Tile<kD>::at(lane & 31, lane >> 5); }
+template <int kD> __device__ __forceinline__ int vt_at(int lane) {
+  const int p = lane & 15;
+  return Tile<kD>::at(4 * (lane >> 5) + (p >> 2), 2 * ((lane >> 4) & 1) + ((p >> 1) & 1)) + 8 * (p & 1);
+}
+// V^T operand of the 16-key step `s`, from the block's offset.  Lane: d 32 db + lane % 32, keys 16 s + 8 jj + 4 h + 0..3.
+template <int kD> __device__ __forceinline__ bf16x8 read_vt(const unsigned char *at, int s) {
+  const bf16x4 x = lds_tr(at + 16 * s * Tile<kD>::kRow), y = lds_tr(at + (16 * s + 8) * Tile<kD>::kRow);
   return (bf16x8)__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 

@@ -199,6 +199,8 @@ int sparrow_chunk_attn(const sparrow_paged_desc *desc, const void *q, const void
   if (B == 0 || n_rows == 0 || max_new == 0) return SPARROW_OK;
   if (int rc = check_table(B, desc->page_size, table_width, table_stride)) return rc;
   if (int rc = check_rows("q_stride_row", desc->q_stride_row, desc->n_q_heads, desc)) return rc;
+  if (n_rows > SPARROW_MAX_PAGED_TOKENS)
+    return fail(SPARROW_ERR_UNSUPPORTED, "n_rows = %d exceeds %d", n_rows, SPARROW_MAX_PAGED_TOKENS);
   if ((int64_t)n_rows * desc->n_q_heads >= 1ll << 31)
     return fail(SPARROW_ERR_UNSUPPORTED, "%d rows of %d heads (less than 2^31)", n_rows, desc->n_q_heads);
   if (!q || !k_cache || !v_cache || !block_table || !cu_new || !kv_len || !out)
