@@ -118,7 +118,11 @@ template <typename T, int kD, int kBM> hipError_t launch(const ChunkArgs &a, hip
 }  // namespace
 
 hipError_t launch_chunk_combine(int dtype, int d, int rows, const ChunkArgs &a, hipStream_t st) {
-  (void)dtype;
+  if (dtype == SPARROW_F32) {
+    if (rows == 16) return d == 128 ? launch<float, 128, 16>(a, st) : launch<float, 64, 16>(a, st);
+    if (rows == 32) return d == 128 ? launch<float, 128, 32>(a, st) : launch<float, 64, 32>(a, st);
+    return d == 128 ? launch<float, 128, 64>(a, st) : launch<float, 64, 64>(a, st);
+  }
   if (rows == 32) return d == 128 ? launch<bf16_t, 128, 32>(a, st) : launch<bf16_t, 64, 32>(a, st);
   if (rows == 64) return d == 128 ? launch<bf16_t, 128, 64>(a, st) : launch<bf16_t, 64, 64>(a, st);
   return d == 128 ? launch<bf16_t, 128, 256>(a, st) : launch<bf16_t, 64, 256>(a, st);
