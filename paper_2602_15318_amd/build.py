@@ -1,5 +1,5 @@
-"""Build the HIP libraries (gfx950) and the binding's native part in-tree: paper_2602_15318_amd/libsparrow.so,
-libsparrow_paged.so, _native.so."""
+"""Build the HIP libraries (gfx950) and the binding's native parts in-tree: paper_2602_15318_amd/libsparrow.so,
+libsparrow_paged.so, _native.so, _native_paged.so."""
 from __future__ import annotations
 
 import concurrent.futures
@@ -15,6 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparrow.so")
 PAGED = os.path.join(HERE, "libsparrow_paged.so")
 NATIVE = os.path.join(HERE, "_native.so")
+NATIVE_PAGED = os.path.join(HERE, "_native_paged.so")
 
 # The preload count puts the leading scalar arguments of a kernel into scalar registers at launch: a
 # wavefront's first load waits for no load of arguments (0.3 to 0.4 us on kernels of 6 to 13 us).
@@ -39,21 +40,25 @@ def _run(cmd, verbose: bool) -> None:
 
 
 def build(verbose: bool = False, extra=()) -> str:
-    """Compile every csrc/*.hip into one shared library, csrc/paged/*.hip into another, and csrc/binding.cpp.  Always recompiles."""
+    """Compile every csrc/*.hip into one shared library, csrc/paged/*.hip into another, and the binding's native
+    part of each.  Always recompiles."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
     def hip(lib, *under):
         srcs = sorted(glob.glob(os.path.join(CSRC, *under, "*.hip")))
         _run([hipcc, *HIPCC_FLAGS, *extra, "-o", lib, *srcs], verbose)
 
-    with concurrent.futures.ThreadPoolExecutor(2) as pool:     # side by side: each is one compiler, file after file
-        for done in [pool.submit(hip, LIB), pool.submit(hip, PAGED, "paged")]:
+    def native(lib, *source):
+        torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+        _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+              "-isystem", os.path.join(torch, "include"), "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+              "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, *source), "-o", lib,
+              "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
+
+    with concurrent.futures.ThreadPoolExecutor(4) as pool:     # side by side: each is one compiler, file after file
+        for done in [pool.submit(hip, LIB), pool.submit(hip, PAGED, "paged"), pool.submit(native, NATIVE, "binding.cpp"),
+                     pool.submit(native, NATIVE_PAGED, "paged", "binding_paged.cpp")]:
             done.result()
-    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
-    _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
-          "-isystem", os.path.join(torch, "include"), "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
-          "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "binding.cpp"), "-o", NATIVE,
-          "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
     return LIB
 
 

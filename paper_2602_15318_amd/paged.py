@@ -3,11 +3,18 @@
 Function names and argument order follow include/sparrow_paged.h.  Tensors are torch tensors on one GPU; only the rotary
 frequencies and their axes are host arrays.  There is no fallback: if the HIP library has not been built, importing this module
 raises.  A call runs on the current stream of its tensors' device, or on `stream`.
+
+Calls whose arguments are plain go through _native_paged.so (csrc/paged/binding_paged.cpp): it does the checks and the marshalling below
+in C++ and returns NotImplemented for everything else.
 """
 from __future__ import annotations
 
 import ctypes
 import os
+import re
+import sys
+import types
+import warnings
 
 import numpy as np
 import torch
@@ -54,6 +61,33 @@ lib = _load()
 def _check(rc: int) -> None:
     if rc != 0:
         raise SparrowError(rc, lib.sparrow_paged_last_error().decode())
+
+
+def _stream_of(index):
+    """The current stream of the GPU `index`, or None where another GPU is the current one."""
+    return torch._C._cuda_getCurrentRawStream(index) if torch._C._cuda_getDevice() == index else None
+
+
+def _load_native():
+    """_native_paged.so; where it is missing, does not load or was built for another torch or Python, functions that leave every
+    call to the code below (which is slower on the host and otherwise the same)."""
+    here = f"torch {re.match('[0-9.]*[0-9]', torch.__version__)[0]}, Python {sys.version_info[0]}.{sys.version_info[1]}"
+    try:
+        from . import _native_paged as native
+        built_for = getattr(native, "BUILT_FOR", "another state of the source")
+        if built_for == here:
+            return native
+        reason = f"was built for {built_for} and this is {here}"
+    except ImportError as e:
+        reason = f"does not load ({e})"
+    warnings.warn(f"_native_paged.so, the paged binding's native part, {reason}: calls take longer on the host.  Build it with "
+                  "`python -m paper_2602_15318_amd.build` (or __graft_entry__.build())", RuntimeWarning, stacklevel=2)
+    calls = ("page_update", "mrope_table", "mrope_append", "chunk_attn")
+    return types.SimpleNamespace(FUNCTIONS=(), setup=lambda *a: None, **{n: lambda *a: NotImplemented for n in calls})
+
+
+_native = _load_native()
+_native.setup(_check, _stream_of, np.ndarray, *(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _native.FUNCTIONS))
 
 
 def _ptr(t):
@@ -146,6 +180,9 @@ def page_update(old_len, new_len, block_table, free_pages, n_free, page_size: in
     """sparrow_page_update: requests from old_len to new_len tokens (int32 [B]); block_table [B, width], free_pages [capacity]
     and n_free [1] are changed in place.  n_rows: the rows that the new tokens are given, at least as many.
     Returns int32 tensors (slots [n_rows], cu_new [B+1], positions [n_rows], status [1]), or fills `outputs`, four such."""
+    r = _native.page_update(old_len, new_len, block_table, free_pages, n_free, page_size, n_rows, pos_offset, outputs, stream)
+    if r is not NotImplemented:
+        return r
     B = old_len.shape[0]
     dev = _tensors(old_len, new_len, block_table, free_pages, n_free, pos_offset, *(outputs or ()))
     _ints("old_len", old_len, B)
@@ -174,6 +211,9 @@ def page_update(old_len, new_len, block_table, free_pages, n_free, page_size: in
 def mrope_table(positions, inv_freq, freq_axis, cos=None, sin=None, stream=None):
     """sparrow_mrope_table.  positions int32 [axes, N] (rows may be one expanded row) or [N]; inv_freq float64 and freq_axis
     int32, host arrays [d/2].  Returns float32 (cos, sin) [N, d/2], the rows that draft_qkv_append takes."""
+    r = _native.mrope_table(positions, inv_freq, freq_axis, cos, sin, stream)
+    if r is not NotImplemented:
+        return r
     N = positions.shape[-1]
     n_axes, stride, inv_freq, freq_axis, d = _axes(positions, N, inv_freq, freq_axis, None)
     dev = _tensors(positions, cos, sin)
@@ -195,6 +235,9 @@ def mrope_append(q, k, v, positions, inv_freq, freq_axis, slots, k_cache, v_cach
     """sparrow_mrope_append.  q [N,Hq,d], k and v [N,Hkv,d] (slices of a fused product may be passed as they are); positions,
     inv_freq, freq_axis as in mrope_table; slots int32 [N]; k_cache, v_cache [n_pages,page_size,Hkv,d] (written in place).
     Returns the rotated q [N,Hq,d]; rows whose slot is outside the cache are left as they were."""
+    r = _native.mrope_append(q, k, v, positions, inv_freq, freq_axis, slots, k_cache, v_cache, q_out, stream)
+    if r is not NotImplemented:
+        return r
     n_pages, page, hkv, d, s_page, s_tok, s_head = _cache(k_cache, v_cache)
     N, hq = q.shape[0], q.shape[1]
     q_row = _rows("q", q, hq, d, k_cache.dtype)
@@ -228,6 +271,9 @@ def chunk_attn(q, k_cache, v_cache, block_table, cu_new, kv_len, max_new: int, s
     """sparrow_chunk_attn.  q [rows,Hq,d] (rows may be apart); k_cache, v_cache [n_pages,page_size,Hkv,d]; block_table int32
     [B,width]; cu_new int32 [B+1] and kv_len int32 [B] on the GPU; max_new: the most new tokens of a request.
     Returns (out, lse); rows behind cu_new[B] are left as they were."""
+    r = _native.chunk_attn(q, k_cache, v_cache, block_table, cu_new, kv_len, max_new, scale, out, lse, want_lse, workspace, stream)
+    if r is not NotImplemented:
+        return r
     n_pages, page, hkv, d, s_page, s_tok, s_head = _cache(k_cache, v_cache)
     B, (rows, hq) = kv_len.shape[0], q.shape[:2]
     q_row = _rows("q", q, hq, d, k_cache.dtype)
