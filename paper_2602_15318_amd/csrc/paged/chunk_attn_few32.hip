@@ -1,4 +1,4 @@
-// Attention of few new tokens over the paged cache, bf16: up to 64 rows (new token, query head of the group) per request and KV head.
+// Attention of few new tokens over the paged cache, bf16: 17 to 64 rows (new token, query head of the group) per request and KV head.
 // Bound by memory: every key and value is read once, by one workgroup.
 //
 // A workgroup of four wavefronts takes one piece of a request's keys for one KV head; the wavefronts take its 32-token tiles in turn
@@ -13,7 +13,7 @@ namespace {
 constexpr int kWaves = 4, kTokens = 32;
 
 template <int kD, int kRT>
-__global__ void __launch_bounds__(64 * kWaves) chunk_few_kernel(ChunkArgs a) {
+__global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
   constexpr int kBM = 32 * kRT, kDB = kD / 32, kKS = kD / 16;
   constexpr int kTileBytes = kTokens * 2 * kD, kLoads = kTokens / Tile<kD>::kLoadRows;   // of a tile of K (or V)
   constexpr int kRowChunks = kD / 4;                       // 16-byte chunks of a row of fp32 outputs
@@ -206,14 +206,14 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few_kernel(ChunkArgs a) {
 
 }  // namespace
 
-hipError_t launch_chunk_few(int d, int rows, const ChunkArgs &a, hipStream_t st) {
+hipError_t launch_chunk_few32(int d, int rows, const ChunkArgs &a, hipStream_t st) {
   const dim3 grid(a.Hkv, a.slots), block(64 * kWaves);
   if (d == 128) {
-    if (rows == 32) hipLaunchKernelGGL((chunk_few_kernel<128, 1>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((chunk_few_kernel<128, 2>), grid, block, 0, st, a);
+    if (rows == 32) hipLaunchKernelGGL((chunk_few32_kernel<128, 1>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((chunk_few32_kernel<128, 2>), grid, block, 0, st, a);
   } else {
-    if (rows == 32) hipLaunchKernelGGL((chunk_few_kernel<64, 1>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((chunk_few_kernel<64, 2>), grid, block, 0, st, a);
+    if (rows == 32) hipLaunchKernelGGL((chunk_few32_kernel<64, 1>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((chunk_few32_kernel<64, 2>), grid, block, 0, st, a);
   }
   return hipGetLastError();
 }

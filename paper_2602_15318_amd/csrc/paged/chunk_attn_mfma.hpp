@@ -92,6 +92,17 @@ __device__ __forceinline__ float pair_sum(float v) {
 __device__ __forceinline__ unsigned int no_numbers(unsigned int w) {
   return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
+// 1.0 in the halves that are infinite of that sign, or NaN
+__device__ __forceinline__ unsigned int ones_of(unsigned int w, bool negative) {
+  unsigned int r = 0u;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const unsigned int x = (w >> (16 * half)) & 0xffffu;
+    const bool no = (x & 0x7f80u) == 0x7f80u, nan = (x & 0x7fu) != 0u;
+    if (no && (nan || ((x & 0x8000u) != 0u) == negative)) r |= 0x3f80u << (16 * half);
+  }
+  return r;
+}
 // O^T += V^T P^T of one operand of a tile in which some rows do not see some keys.  0 * inf must not reach those rows, so what is no number
 // leaves the operand; whether a row sees one such value or more is counted by products of ones, exactly, and adds the infinities then (a NaN
 // counts as both).
@@ -104,16 +115,8 @@ __device__ __forceinline__ f32x16 add_masked(bf16x8 v, bf16x8 p, bf16x8 seen, f3
   u32x4 up, down;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    unsigned int u = 0u, d = 0u;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const unsigned int x = (w[i] >> (16 * half)) & 0xffffu;
-      const bool no = (x & 0x7f80u) == 0x7f80u, nan = no && (x & 0x7fu) != 0u;
-      if (no && (nan || (x & 0x8000u) == 0u)) u |= 0x3f80u << (16 * half);      // 1.0
-      if (no && (nan || (x & 0x8000u) != 0u)) d |= 0x3f80u << (16 * half);
-    }
-    up[i] = u;
-    down[i] = d;
+    up[i] = ones_of(w[i], false);
+    down[i] = ones_of(w[i], true);
     w[i] &= ~bad[i];
   }
   o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p, o, 0, 0, 0);

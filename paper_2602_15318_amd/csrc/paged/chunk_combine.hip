@@ -1,15 +1,16 @@
-// Second pass of the chunk attention: the pieces of a block's keys put together.  kSpread wavefronts (4, or 1 where there are many
-// rows) share the pieces of one (row of the batch, query head), all loads of a wavefront on their way at once.
+// Second pass of the chunk attention: the pieces of a block's keys put together.  kSpread wavefronts (16, 4, or 1: the more rows, the
+// fewer) share the pieces of one (row of the batch, query head), all loads of a wavefront on their way at once.
 #include "chunk_plan.hpp"
 
 namespace sparrow {
 
 namespace {
 
-constexpr int kWaves = 4, kAtOnce = 8;
+constexpr int kAtOnce = 8;
 
 template <typename T, int kD, int kBM, int kSpread>
-__global__ void __launch_bounds__(64 * kWaves) chunk_combine_kernel(ChunkArgs a) {
+__global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combine_kernel(ChunkArgs a) {
+  constexpr int kWaves = kSpread == 1 ? 4 : kSpread;
   constexpr int kPer = kD / 64;                            // floats of a lane
   __shared__ float sum_o[kWaves][kD], sum_l[kWaves], tops[kWaves];
   const int lane = threadIdx.x & 63;
@@ -105,26 +106,26 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_combine_kernel(ChunkArgs a)
 }
 
 template <typename T, int kD, int kBM> hipError_t launch(const ChunkArgs &a, hipStream_t st) {
-  const dim3 block(64 * kWaves);
   const int y = a.n_rows < 32768 ? a.n_rows : 32768, z = (a.n_rows + 32767) / 32768;
-  // four wavefronts a (row, head) while that leaves the chip's wavefronts unfilled
-  if ((int64_t)a.n_rows * a.Hq <= 2048)
-    hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, kWaves>), dim3(a.Hq, y, z), block, 0, st, a);
-  else
-    hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, 1>), dim3(1, y, z), block, 0, st, a);
+  // as many wavefronts a (row, head) as the chip holds
+  const int64_t rows = (int64_t)a.n_rows * a.Hq;
+  if (rows <= 512) hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, 16>), dim3(a.Hq, y, z), dim3(1024), 0, st, a);
+  else if (rows <= 2048) hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, 4>), dim3(a.Hq, y, z), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, 1>), dim3(1, y, z), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_chunk_combine(int dtype, int d, int rows, const ChunkArgs &a, hipStream_t st) {
-  if (dtype == SPARROW_F32) {
-    if (rows == 16) return d == 128 ? launch<float, 128, 16>(a, st) : launch<float, 64, 16>(a, st);
-    if (rows == 32) return d == 128 ? launch<float, 128, 32>(a, st) : launch<float, 64, 32>(a, st);
-    return d == 128 ? launch<float, 128, 64>(a, st) : launch<float, 64, 64>(a, st);
-  }
-  if (rows == 32) return d == 128 ? launch<bf16_t, 128, 32>(a, st) : launch<bf16_t, 64, 32>(a, st);
-  if (rows == 64) return d == 128 ? launch<bf16_t, 128, 64>(a, st) : launch<bf16_t, 64, 64>(a, st);
+  const bool f32 = dtype == SPARROW_F32;
+#define SPARROW_ROWS(n) \
+  if (rows == n && f32) return d == 128 ? launch<float, 128, n>(a, st) : launch<float, 64, n>(a, st); \
+  if (rows == n) return d == 128 ? launch<bf16_t, 128, n>(a, st) : launch<bf16_t, 64, n>(a, st);
+  SPARROW_ROWS(16)
+  SPARROW_ROWS(32)
+  SPARROW_ROWS(64)
+#undef SPARROW_ROWS
   return d == 128 ? launch<bf16_t, 128, 256>(a, st) : launch<bf16_t, 64, 256>(a, st);
 }
 

@@ -2,9 +2,8 @@
 // plan out themselves, each the same one: a wavefront holds a request per lane (and register, above 64 requests).
 //
 // A row is a (new token, query head of the group) pair; the rows of a request and KV head are cut into blocks of kBM rows, a
-// block's keys into pieces.  With N pieces to hand out per KV head and U blocks in the batch, pieces are of
-// T = sum(blocks * length) / (N - U) tokens at most: the sum over the blocks of ceil(length / T) is then at most N.  Blocks
-// are not cut at all where N is not above U.
+// block's keys into pieces of T tokens at most, T as small as it may be for the sum over the blocks of ceil(length / T) to be at
+// most N, the pieces per KV head of the call.  Blocks are not cut at all where N is not above their number U.
 #pragma once
 #include "paged.hpp"
 
@@ -60,6 +59,7 @@ struct Plan {
   int T, n_blocks[kMaxPerLane], n_splits[kMaxPerLane], end[kMaxPerLane];
   Request rq[kMaxPerLane];
 };
+__device__ __forceinline__ int splits_of(int L, int T) { return quotient(max(L - 1, 0), T, __builtin_amdgcn_rcpf((float)T)) + 1; }
 // Lane l's requests l, l + 64, ...
 template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a, int lane) {
   Plan p;
@@ -81,16 +81,32 @@ template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a,
   const int U = lane_value(wave_scan(blocks), 63);
   const float W = wave_sum_valu(weight);
   p.T = 1 << 30;
-  // (the factor: the sum is off by 2^-16 at most)
-  if (a.slots > U) p.T = (min((int)(W * (1.f + 0x1p-14f) / (float)(a.slots - U)), 1 << 29) + kGrain) / kGrain * kGrain;
-  const float inv_T = __builtin_amdgcn_rcpf((float)p.T);
+  if (a.slots > U) {
+    // T1 = W / (N - U) always fits; the smallest that does lies between W / N and it, and is looked for where they differ by much.
+    // (the factor: the sum is off by 2^-16 at most)
+    const auto grains = [&](float t) { return (min((int)(t * (1.f + 0x1p-14f)), 1 << 29) + kGrain) / kGrain; };
+    int hi = grains(W / (float)(a.slots - U));
+    if (a.slots < 8 * U) {
+      int lo = max(grains(W / (float)a.slots) - 1, 0);       // (lo: too small, or not tried)
+      for (int step = 0; step < 6 && hi - lo > 1; ++step) {
+        const int mid = (lo + hi) >> 1;
+        int sum = 0;
+#pragma unroll
+        for (int k = 0; k < kMaxPerLane; ++k)
+          if (64 * k < a.B) sum += min(p.n_blocks[k], a.slots) * splits_of(p.rq[k].L, mid * kGrain);
+        if (lane_value(wave_scan(sum), 63) <= a.slots) hi = mid;
+        else lo = mid;
+      }
+    }
+    p.T = hi * kGrain;
+  }
   int before = 0;
 #pragma unroll
   for (int k = 0; k < kMaxPerLane; ++k) {
     p.n_splits[k] = 1;
     p.end[k] = before;
     if (64 * k < a.B) {
-      p.n_splits[k] = quotient(max(p.rq[k].L - 1, 0), p.T, inv_T) + 1;
+      p.n_splits[k] = splits_of(p.rq[k].L, p.T);
       p.end[k] = before + wave_scan(p.n_blocks[k] * p.n_splits[k]);
       before = lane_value(p.end[k], 63);
     }
