@@ -1,5 +1,5 @@
-// Attention of new tokens over the paged cache by 16-row tiles: bf16 up to 16 rows (new token, query head of the group) per request and KV head,
-// fp32 any number, in blocks of 16, 32 or 64.  Bound by memory (fp32 above 32 rows by the matrix cores: 157 TFLOP/s).
+// Attention of few new tokens over the paged cache by 16-row tiles: up to 16 rows (new token, query head of the group) per request and KV head, in
+// fp32 up to 32.  Bound by memory.
 //
 // A workgroup takes one block and piece of keys; its wavefronts take the 16-token tiles in turn and know nothing of each other until the
 // end, where their states of a row are merged through LDS.  A tile lies on one page; it travels memory -> LDS past the registers, two
@@ -11,52 +11,13 @@
 //                 ones, step i taking keys 4 c4 + i (fp32).
 #include <type_traits>
 
-#include "chunk_attn_mfma.hpp"
+#include "chunk_attn_16.hpp"
 
 namespace sparrow {
 
 namespace {
 
 constexpr int kTokens = 16;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-
-// Over lanes l, l ^ 16, l ^ 32, l ^ 48
-__device__ __forceinline__ float quad_max(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return pair_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
-}
-__device__ __forceinline__ float quad_sum(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
-}
-
-__device__ __forceinline__ f32x4 mul16(bf16x4 v, bf16x4 p, f32x4 o) {
-  return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, v), __builtin_bit_cast(s16x4, p), o, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 infinities(f32x4 o, f32x4 up, f32x4 down) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] += (up[i] > 0.f ? INFINITY : 0.f) + (down[i] > 0.f ? -INFINITY : 0.f);
-  return o;
-}
-// As add_masked (chunk_attn_mfma.hpp): a product of a tile in which some rows do not see some keys.
-__device__ __forceinline__ f32x4 add_masked16(bf16x4 v, bf16x4 p, bf16x4 seen, f32x4 o) {
-  u32x2 w = __builtin_bit_cast(u32x2, v);
-  const u32x2 bad = {no_numbers(w[0]), no_numbers(w[1])};
-  if (__builtin_amdgcn_ballot_w64((bad[0] | bad[1]) != 0u) == 0ull) return mul16(v, p, o);
-  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  const u32x2 up = {ones_of(w[0], false), ones_of(w[1], false)}, down = {ones_of(w[0], true), ones_of(w[1], true)};
-  w &= ~bad;
-  return infinities(mul16(__builtin_bit_cast(bf16x4, w), p, o), mul16(__builtin_bit_cast(bf16x4, up), seen, zero),
-                    mul16(__builtin_bit_cast(bf16x4, down), seen, zero));
-}
-__device__ __forceinline__ f32x4 add_masked4(float v, float p, float seen, f32x4 o) {
-  const bool no = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u, nan = v != v;
-  if (__builtin_amdgcn_ballot_w64(no) == 0ull) return __builtin_amdgcn_mfma_f32_16x16x4f32(v, p, o, 0, 0, 0);
-  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  return infinities(__builtin_amdgcn_mfma_f32_16x16x4f32(no ? 0.f : v, p, o, 0, 0, 0),
-                    __builtin_amdgcn_mfma_f32_16x16x4f32(nan || (no && v > 0.f) ? 1.f : 0.f, seen, zero, 0, 0, 0),
-                    __builtin_amdgcn_mfma_f32_16x16x4f32(nan || (no && v < 0.f) ? 1.f : 0.f, seen, zero, 0, 0, 0));
-}
 
 template <typename T, int kD, int kRT, int kWaves>
 __global__ void __launch_bounds__(64 * kWaves) chunk_few16_kernel(ChunkArgs a) {
@@ -185,29 +146,40 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few16_kernel(ChunkArgs a) {
       if (more2) wait_loads<3 * kLoads>();
       else if (more) wait_loads<2 * kLoads>();
       else wait_loads<0>();
-#pragma unroll
-      for (int db = 0; db < kDB; ++db) {
+      auto output = [&](auto masked) __attribute__((always_inline)) {
+        constexpr bool kMasked = decltype(masked)::value;
         if constexpr (kF32) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float v = *reinterpret_cast<const float *>(V + (4 * c4 + i) * kRow + (16 * db + n16) * 4);
+          for (int db = 0; db < kDB; ++db)
 #pragma unroll
-            for (int rt = 0; rt < kRT; ++rt)
-              o[rt][db] = edge ? add_masked4(v, p[rt][i], seen[rt][i], o[rt][db])
-                               : __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[rt][i], o[rt][db], 0, 0, 0);
-          }
+            for (int i = 0; i < 4; ++i) {
+              const float v = *reinterpret_cast<const float *>(V + (4 * c4 + i) * kRow + (16 * db + n16) * 4);
+#pragma unroll
+              for (int rt = 0; rt < kRT; ++rt)
+                o[rt][db] = kMasked ? add_masked4(v, p[rt][i], seen[rt][i], o[rt][db])
+                                    : __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[rt][i], o[rt][db], 0, 0, 0);
+            }
         } else {
           // probabilities are rounded to bf16 for the product (their sum is not): 2^-9 of a term on average, of the result less
-          const int row = 4 * c4 + (n16 >> 2), chunk = 2 * db + ((n16 >> 1) & 1);
-          const bf16x4 v = lds_tr(V + row * kRow + ((chunk ^ swz(row)) << 4) + 8 * (n16 & 1));
+          bf16x4 pb[kRT], ones[kRT];
 #pragma unroll
-          for (int rt = 0; rt < kRT; ++rt) {
-            const bf16x4 pb = {(__bf16)p[rt][0], (__bf16)p[rt][1], (__bf16)p[rt][2], (__bf16)p[rt][3]};
-            const bf16x4 ones = {(__bf16)seen[rt][0], (__bf16)seen[rt][1], (__bf16)seen[rt][2], (__bf16)seen[rt][3]};
-            o[rt][db] = edge ? add_masked16(v, pb, ones, o[rt][db]) : mul16(v, pb, o[rt][db]);
+          for (int rt = 0; rt < kRT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              pb[rt][i] = (__bf16)p[rt][i];
+              if (kMasked) ones[rt][i] = (__bf16)seen[rt][i];
+            }
+          const int row = 4 * c4 + (n16 >> 2);
+#pragma unroll
+          for (int db = 0; db < kDB; ++db) {
+            const bf16x4 v = lds_tr(V + row * kRow + (((2 * db + ((n16 >> 1) & 1)) ^ swz(row)) << 4) + 8 * (n16 & 1));
+#pragma unroll
+            for (int rt = 0; rt < kRT; ++rt) o[rt][db] = kMasked ? add_masked16(v, pb[rt], ones[rt], o[rt][db]) : mul16(v, pb[rt], o[rt][db]);
           }
         }
-      }
+      };
+      if (edge) output(std::true_type());
+      else output(std::false_type());
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more2) issue(Vg, !kF32, w + (it + 2) * kWaves, 2 * buf + 1);
     }
@@ -274,7 +246,7 @@ template <typename T, int kRT, int kWaves> hipError_t launch(int d, dim3 grid, c
 hipError_t launch_chunk_few16(int dtype, int d, int rows, int blocks, const ChunkArgs &a, hipStream_t st) {
   const dim3 grid(a.Hkv, blocks < 32768 ? blocks : 32768, (blocks + 32767) / 32768);
   if (dtype == SPARROW_F32)
-    return rows == 16 ? launch<float, 1, 4>(d, grid, a, st) : rows == 32 ? launch<float, 2, 4>(d, grid, a, st) : launch<float, 4, 4>(d, grid, a, st);
+    return rows == 16 ? launch<float, 1, 4>(d, grid, a, st) : launch<float, 2, 4>(d, grid, a, st);
   return launch<bf16_t, 1, 4>(d, grid, a, st);
 }
 

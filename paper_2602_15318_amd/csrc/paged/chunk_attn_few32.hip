@@ -4,6 +4,8 @@
 // A workgroup of four wavefronts takes one piece of a request's keys for one KV head; the wavefronts take its 32-token tiles in turn
 // and know nothing of each other until the end, where their four states of a row are merged through LDS.  A wavefront's tiles travel
 // memory -> LDS without passing registers (page by page, two tiles of K and V ahead, 64 KB in flight on a compute unit).
+#include <type_traits>
+
 #include "chunk_attn_mfma.hpp"
 
 namespace sparrow {
@@ -138,16 +140,20 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
       if (more2) wait_loads<3 * kLoads>();
       else if (more) wait_loads<2 * kLoads>();
       else wait_loads<0>();
+      auto output = [&](auto masked) __attribute__((always_inline)) {
 #pragma unroll
-      for (int db = 0; db < kDB; ++db)
+        for (int db = 0; db < kDB; ++db)
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          const bf16x8 v = read_vt<kD>(V + (vt_at<kD>(lane) ^ db << 6), st);
+          for (int st = 0; st < 2; ++st) {
+            const bf16x8 v = read_vt<kD>(V + (vt_at<kD>(lane) ^ db << 6), st);
 #pragma unroll
-          for (int rt = 0; rt < kRT; ++rt)
-            o[rt][db] = edge ? add_masked(v, pb[rt][st], seen[rt][st], o[rt][db])
-                             : __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[rt][st], o[rt][db], 0, 0, 0);
-        }
+            for (int rt = 0; rt < kRT; ++rt)
+              o[rt][db] = decltype(masked)::value ? add_masked(v, pb[rt][st], seen[rt][st], o[rt][db])
+                                                  : __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[rt][st], o[rt][db], 0, 0, 0);
+          }
+      };
+      if (edge) output(std::true_type());
+      else output(std::false_type());
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more2) issue(pages.v, w + (it + 2) * kWaves, 2 * buf + 1);
     }
@@ -171,6 +177,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
   }
   __syncthreads();
   const bool direct = pc.n_splits == 1;
+  if (!direct && idx >= a.slots) return;                   // (offsets that overlap)
   const int64_t part = ((int64_t)idx * a.Hkv + c) * kBM;
   for (int x = threadIdx.x; x < R * kRowChunks; x += 64 * kWaves) {
     const int r = x / kRowChunks, chunk = x % kRowChunks;
@@ -206,8 +213,8 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
 
 }  // namespace
 
-hipError_t launch_chunk_few32(int d, int rows, const ChunkArgs &a, hipStream_t st) {
-  const dim3 grid(a.Hkv, a.slots), block(64 * kWaves);
+hipError_t launch_chunk_few32(int d, int rows, int blocks, const ChunkArgs &a, hipStream_t st) {
+  const dim3 grid(a.Hkv, blocks), block(64 * kWaves);
   if (d == 128) {
     if (rows == 32) hipLaunchKernelGGL((chunk_few32_kernel<128, 1>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((chunk_few32_kernel<128, 2>), grid, block, 0, st, a);

@@ -13,12 +13,6 @@ namespace {
 
 constexpr int kWaves = 8, kTokens = 64, kBM = 256, kStages = 4;
 
-__device__ __forceinline__ void barrier() {
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-}
-
 template <int kD>
 __global__ void __launch_bounds__(64 * kWaves, 2) chunk_many_kernel(ChunkArgs a) {
   constexpr int kDB = kD / 32, kKS = kD / 16, kHalf = kKS / 2;

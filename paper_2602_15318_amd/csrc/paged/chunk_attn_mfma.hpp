@@ -62,6 +62,13 @@ __device__ __forceinline__ Pages pages_of(const ChunkArgs &a, const Piece &pc, i
   return p;
 }
 
+// The wavefront's LDS reads and writes are done before the barrier; its loads to LDS are not waited for.
+__device__ __forceinline__ void barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 __device__ __forceinline__ bf16x8 lds_b128(const unsigned char *p) { return *reinterpret_cast<const bf16x8 *>(p); }
 __device__ __forceinline__ bf16x4 lds_tr(const unsigned char *p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)p);

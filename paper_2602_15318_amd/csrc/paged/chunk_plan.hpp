@@ -3,7 +3,8 @@
 //
 // A row is a (new token, query head of the group) pair; the rows of a request and KV head are cut into blocks of kBM rows, a
 // block's keys into pieces of T tokens at most, T as small as it may be for the sum over the blocks of ceil(length / T) to be at
-// most N, the pieces per KV head of the call.  Blocks are not cut at all where N is not above their number U.
+// most N, the pieces per KV head that the chip holds at once, or twice that if two rounds of shorter pieces end sooner.  Blocks are not cut
+// at all where N is not above their number U.
 #pragma once
 #include "paged.hpp"
 
@@ -81,24 +82,31 @@ template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a,
   const int U = lane_value(wave_scan(blocks), 63);
   const float W = wave_sum_valu(weight);
   p.T = 1 << 30;
-  if (a.slots > U) {
+  int best = 1 << 30;
+  for (int round = 1; round * a.round <= a.slots; ++round) {
+    const int N = round * a.round;
+    if (N <= U) continue;
     // T1 = W / (N - U) always fits; the smallest that does lies between W / N and it, and is looked for where they differ by much.
     // (the factor: the sum is off by 2^-16 at most)
     const auto grains = [&](float t) { return (min((int)(t * (1.f + 0x1p-14f)), 1 << 29) + kGrain) / kGrain; };
-    int hi = grains(W / (float)(a.slots - U));
-    if (a.slots < 8 * U) {
-      int lo = max(grains(W / (float)a.slots) - 1, 0);       // (lo: too small, or not tried)
+    int hi = grains(W / (float)(N - U));
+    if (N < 8 * U) {
+      int lo = max(grains(W / (float)N) - 1, 0);             // (lo: too small, or not tried)
       for (int step = 0; step < 6 && hi - lo > 1; ++step) {
         const int mid = (lo + hi) >> 1;
         int sum = 0;
 #pragma unroll
         for (int k = 0; k < kMaxPerLane; ++k)
           if (64 * k < a.B) sum += min(p.n_blocks[k], a.slots) * splits_of(p.rq[k].L, mid * kGrain);
-        if (lane_value(wave_scan(sum), 63) <= a.slots) hi = mid;
+        if (lane_value(wave_scan(sum), 63) <= N) hi = mid;
         else lo = mid;
       }
     }
-    p.T = hi * kGrain;
+    const int cost = round * (hi + 4);                       // (a piece's beginning and end take as long as four grains)
+    if (cost < best) {
+      best = cost;
+      p.T = hi * kGrain;
+    }
   }
   int before = 0;
 #pragma unroll

@@ -45,16 +45,16 @@ struct ChunkArgs {
   float *lse;
   int64_t table_stride, q_row, stride_page, stride_token, stride_head;          // elements
   int32_t B, n_rows, max_new, Hq, Hkv, g, table_width, page_shift, n_pages;
-  int32_t slots;           // pieces per KV head that the blocks of rows may be cut into; 0: one piece each
+  int32_t slots, round;    // pieces per KV head that the blocks of rows may be cut into (0: one piece each); those that run at once
   float scale_log2, inv_g;
   float *part_o, *part_ml; // [piece * Hkv + KV head][row of the block]: unnormalised output [d]; reference point (log2), sum
 };
 // How a call of these sizes is run: rows per block, blocks of the batch at most, pieces per KV head, floats of part_o and part_ml.
 struct ChunkShape {
-  int rows, blocks, slots;
+  int rows, blocks, slots, round;
   int64_t floats_o, floats_ml;
 };
-ChunkShape chunk_shape(int dtype, int d, int Hq, int Hkv, int B, int64_t n_rows, int max_new);
+ChunkShape chunk_shape(int dtype, int d, int Hq, int Hkv, int B, int64_t n_rows, int max_new, int64_t capacity);
 hipError_t launch_chunk_attn(int dtype, int d, const ChunkArgs &a, hipStream_t st);
 
 }  // namespace sparrow

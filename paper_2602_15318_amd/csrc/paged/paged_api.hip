@@ -184,7 +184,7 @@ size_t sparrow_chunk_attn_workspace(const sparrow_paged_desc *desc, int32_t B, i
   if (!desc || desc->n_q_heads <= 0 || desc->n_kv_heads <= 0 || desc->n_q_heads % desc->n_kv_heads != 0 || B <= 0 || n_rows <= 0 ||
       max_new <= 0)
     return 0;
-  const ChunkShape s = chunk_shape(desc->dtype, desc->head_dim, desc->n_q_heads, desc->n_kv_heads, B, n_rows, max_new);
+  const ChunkShape s = chunk_shape(desc->dtype, desc->head_dim, desc->n_q_heads, desc->n_kv_heads, B, n_rows, max_new, SPARROW_MAX_PAGED_TOKENS);
   return round_up((size_t)s.floats_o * 4, 256) + round_up((size_t)s.floats_ml * 4, 256);
 }
 
@@ -222,8 +222,8 @@ int sparrow_chunk_attn(const sparrow_paged_desc *desc, const void *q, const void
   a.table_width = table_width; a.page_shift = shift_of(desc->page_size); a.n_pages = desc->n_pages;
   a.scale_log2 = (desc->scale > 0.f ? desc->scale : 1.0f / std::sqrt((float)desc->head_dim)) * kLog2e;
   a.inv_g = 1.0f / (float)a.g;
-  const ChunkShape shape = chunk_shape(desc->dtype, desc->head_dim, a.Hq, a.Hkv, B, n_rows, max_new);
-  a.slots = shape.slots;
+  const ChunkShape shape = chunk_shape(desc->dtype, desc->head_dim, a.Hq, a.Hkv, B, n_rows, max_new, (int64_t)table_width * desc->page_size);
+  a.slots = shape.slots; a.round = shape.round;
   a.part_o = (float *)workspace;
   a.part_ml = (float *)((unsigned char *)workspace + round_up((size_t)shape.floats_o * 4, 256));
   const hipError_t e = launch_chunk_attn(desc->dtype, desc->head_dim, a, (hipStream_t)hip_stream);
