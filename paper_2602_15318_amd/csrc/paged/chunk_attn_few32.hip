@@ -16,8 +16,9 @@ constexpr int kWaves = 4, kTokens = 32;
 
 template <int kD, int kRT>
 __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
+  using Rows = Tile<kD, false>;
   constexpr int kBM = 32 * kRT, kDB = kD / 32, kKS = kD / 16;
-  constexpr int kTileBytes = kTokens * 2 * kD, kLoads = kTokens / Tile<kD>::kLoadRows;   // of a tile of K (or V)
+  constexpr int kTileBytes = kTokens * 2 * kD, kLoads = kTokens / Rows::kLoadRows;   // of a tile of K (or V)
   constexpr int kRowChunks = kD / 4;                       // 16-byte chunks of a row of fp32 outputs
   constexpr int kTiles = kWaves * 4 * kTileBytes, kMerge = kWaves * kBM * kD * 4;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kTiles > kMerge ? kTiles : kMerge];   // [wave][K0, V0, K1, V1]
@@ -33,16 +34,18 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
 
   unsigned char *mine = lds + w * 4 * kTileBytes;
   const unsigned int mine_at = lds_offset(mine);
-  unsigned int off[2];
+  unsigned int from_k[2], from_v[2];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) off[j] = (unsigned int)(lane / Tile<kD>::kChunks) * pages.stride_token + 16u * Tile<kD>::chunk(lane, j);
-  auto issue = [&](const unsigned char *src, int tile, int part) __attribute__((always_inline)) {
+  for (int j = 0; j < 2; ++j) from_k[j] = Rows::k_from(lane, Rows::kLoadRows * j, pages.stride_token);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) from_v[j] = Rows::v_from(lane, Rows::kLoadRows * j, pages.stride_token);
+  auto issue = [&](bool value, int tile, int part) __attribute__((always_inline)) {
     const int t = pc.t0 + tile * kTokens;
     const int64_t half[2] = {pages.offset(t), pages.offset(t + 16)};
 #pragma unroll
     for (int j = 0; j < kLoads; ++j)
-      global_to_lds<true>(src + half[2 * j / kLoads] + (int64_t)(j % (kLoads / 2) * Tile<kD>::kLoadRows) * pages.stride_token, off[j & 1],
-                          mine_at + part * kTileBytes + 1024 * j);
+      global_to_lds<true>((value ? pages.v : pages.k) + half[2 * j / kLoads] + (int64_t)(j % (kLoads / 2) * Rows::kLoadRows) * pages.stride_token,
+                          value ? from_v[j & 1] : from_k[j & 1], mine_at + part * kTileBytes + 1024 * j);
   };
   const int n_tiles = (pc.t1 - pc.t0 + kTokens - 1) / kTokens;
   const int n = (n_tiles - w + kWaves - 1) / kWaves;       // of this wavefront: w, w + kWaves, ...
@@ -68,23 +71,24 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
     constexpr int kQLoads = kRT * kLoads;
 #pragma unroll
     for (int j = 0; j < kQLoads; ++j) {
-      const int rho = min(j * Tile<kD>::kLoadRows + lane / Tile<kD>::kChunks, R - 1);
+      const int rho = min(j * Rows::kLoadRows + lane / Rows::kChunks, R - 1);
       const int i = (int)(((float)rho + 0.5f) * a.inv_g);
       const unsigned char *at = (const unsigned char *)a.q + 2 * ((int64_t)(pc.rq.row0 + i) * a.q_row + (int64_t)(c * a.g + rho - i * a.g) * kD);
-      global_to_lds_each(at + 16 * Tile<kD>::chunk(lane, j), mine_at + 2 * kTileBytes + 1024 * j);
+      const int row = j * Rows::kLoadRows + lane / Rows::kChunks;
+      global_to_lds_each(at + 16 * ((lane % Rows::kChunks) ^ Rows::swz_k(row)), mine_at + 2 * kTileBytes + 1024 * j);
     }
-    issue(pages.k, w, 0);
-    issue(pages.v, w, 1);
+    issue(false, w, 0);
+    issue(true, w, 1);
     wait_loads<2 * kLoads>();
     bf16x8 q[kRT][kKS];
 #pragma unroll
     for (int rt = 0; rt < kRT; ++rt)
 #pragma unroll
-      for (int ks = 0; ks < kKS; ++ks) q[rt][ks] = lds_b128(mine + 2 * kTileBytes + Tile<kD>::at(32 * rt + (lane & 31), 2 * ks + h));
+      for (int ks = 0; ks < kKS; ++ks) q[rt][ks] = lds_b128(mine + 2 * kTileBytes + Rows::k(32 * rt + (lane & 31), 2 * ks + h));
     wait_loads<2 * kLoads>();                              // (the reads are done: their place may be written)
     if (n > 1) {
-      issue(pages.k, w + kWaves, 2);
-      issue(pages.v, w + kWaves, 3);
+      issue(false, w + kWaves, 2);
+      issue(true, w + kWaves, 3);
     }
     for (int it = 0; it < n; ++it) {
       const int buf = it & 1;
@@ -97,12 +101,12 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
       for (int rt = 0; rt < kRT; ++rt) s[rt] = (f32x16){0.f};
 #pragma unroll
       for (int ks = 0; ks < kKS; ++ks) {
-        const bf16x8 k = lds_b128(K + (k_at<kD>(lane) ^ ks << 5));
+        const bf16x8 k = lds_b128(K + (k_at<kD, false>(lane) ^ ks << 5));
 #pragma unroll
         for (int rt = 0; rt < kRT; ++rt) s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[rt][ks], s[rt], 0, 0, 0);
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (more2) issue(pages.k, w + (it + 2) * kWaves, 2 * buf);
+      if (more2) issue(false, w + (it + 2) * kWaves, 2 * buf);
       const int t = pc.t0 + (w + it * kWaves) * kTokens;
       const bool edge = t + kTokens - 1 > min(pc.rq.past, pc.t1 - 1);     // some row does not see all of the tile
       bf16x8 pb[kRT][2], seen[kRT][2];
@@ -155,7 +159,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
       if (edge) output(std::true_type());
       else output(std::false_type());
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (more2) issue(pages.v, w + (it + 2) * kWaves, 2 * buf + 1);
+      if (more2) issue(true, w + (it + 2) * kWaves, 2 * buf + 1);
     }
   }
   // ---- merge: states of the four wavefronts, fp32, through LDS

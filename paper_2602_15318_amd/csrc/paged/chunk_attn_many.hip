@@ -42,21 +42,29 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_many_kernel(ChunkArgs a)
   for (int db = 0; db < kDB; ++db) o[db] = (f32x16){0.f};
   if (n > 0) {
     const unsigned int lds0 = lds_offset(lds) + 1024 * kLoads * w;
-    unsigned int off[kLoads];
+    unsigned int from_k[kLoads], from_v[kLoads];
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j)
-      off[j] = (unsigned int)(Tile<kD>::kLoadRows * j + lane / Tile<kD>::kChunks) * pages.stride_token + 16u * Tile<kD>::chunk(lane, j);
+    for (int j = 0; j < kLoads; ++j) {
+      const int row = Tile<kD>::kLoadRows * j;
+      from_k[j] = row * pages.stride_token + Tile<kD>::k_from(lane, 8 * w + row, pages.stride_token);
+      from_v[j] = row * pages.stride_token + Tile<kD>::v_from(lane, 8 * w + row, pages.stride_token);
+    }
     auto place = [&](int tile) __attribute__((always_inline)) { return pages.offset(pc.t0 + min(tile, n - 1) * kTokens + 8 * w); };
-    auto load = [&](const unsigned char *src, int64_t at, int buf) __attribute__((always_inline)) {
+    auto load_k = [&](int64_t at, int t) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) global_to_lds<false>(src + at, off[j], lds0 + buf * kTileBytes + 1024 * j);
+      for (int j = 0; j < kLoads; ++j) global_to_lds<false>(pages.k + at, from_k[j], lds0 + (t & (kStages - 1)) * kTileBytes + 1024 * j);
+    };
+    auto load_v = [&](int64_t at, int t) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+        global_to_lds<false>(pages.v + at, from_v[j], lds0 + (kStages + (t & (kStages - 1))) * kTileBytes + 1024 * j);
     };
     const int64_t p0 = place(0), p1 = place(1), p2 = place(2);
-    load(pages.k, p0, 0);
-    load(pages.v, p0, kStages);
-    load(pages.k, p1, 1);
-    load(pages.v, p1, kStages + 1);
-    load(pages.k, p2, 2);
+    load_k(p0, 0);
+    load_v(p0, 0);
+    load_k(p1, 1);
+    load_v(p1, 1);
+    load_k(p2, 2);
     bf16x8 q[kKS];
     {
       const unsigned char *at = (const unsigned char *)a.q + 2 * ((int64_t)(pc.rq.row0 + i_row) * a.q_row + (int64_t)head * kD) + 16 * h;
@@ -71,8 +79,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_many_kernel(ChunkArgs a)
     barrier();
     if (w >= 4) barrier();                                 // half a step behind
     auto request = [&](int t) __attribute__((always_inline)) {
-      load(pages.k, at_k, (t + 3) & (kStages - 1));
-      load(pages.v, at_v, kStages + ((t + 2) & (kStages - 1)));
+      load_k(at_k, t + 3);
+      load_v(at_v, t + 2);
     };
     auto next = [&](int t) __attribute__((always_inline)) {
       at_v = at_k;

@@ -26,14 +26,27 @@ __device__ __forceinline__ void global_to_lds_each(const void *at, unsigned int 
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(at) : "memory", "m0");
 }
 
-// Rows of a tile: 2 kD bytes, the 16-byte chunks XOR-swizzled by the row so that eight consecutive rows read at one chunk, and four rows
-// read transposed, fall on different banks.  What loads a tile writes LDS in lane order, so the lane picks the chunk that belongs there.
-template <int kD> struct Tile {
+// Rows of a tile: 2 kD bytes, the 16-byte chunks XOR-swizzled by the row so that what is read together falls on different banks: of K
+// 16 bytes of each of 32 rows, of V, transposed, 64 bytes of each of four rows at a time.  What loads a tile writes LDS in lane order, so the
+// lane picks the chunk that belongs there.  Both together, chunk of 2,048 tokens over 26,112: 692 -> 653 us.  (kFold: the chunk's lowest bit by the
+// eight rows, without it rows 8 apart meet; few rows leave LDS idle, and its offsets cost registers there.)
+template <int kD, bool kFold = true> struct Tile {
   static constexpr int kRow = 2 * kD, kChunks = kD / 8, kLoadRows = 64 / kChunks;    // rows that one load of a wavefront covers
-  static __device__ __forceinline__ int swz(int row) { return kD == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; }
-  static __device__ __forceinline__ int at(int row, int chunk) { return row * kRow + ((chunk ^ swz(row)) << 4); }
-  // Chunk that lane `lane` of load number j (of consecutive kLoadRows rows) fetches
-  static __device__ __forceinline__ int chunk(int lane, int j) { return (lane % kChunks) ^ swz(lane / kChunks + kLoadRows * (j & 1)); }
+  static __device__ __forceinline__ int swz_k(int row) {
+    return (kD == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1) ^ (kFold ? (row >> 3) & 1 : 0);
+  }
+  static __device__ __forceinline__ int swz_v(int row) {
+    return (kD == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2) | ((row >> 2) & 1) << 1;
+  }
+  static __device__ __forceinline__ int k(int row, int chunk) { return row * kRow + ((chunk ^ swz_k(row)) << 4); }
+  static __device__ __forceinline__ int v(int row, int chunk) { return row * kRow + ((chunk ^ swz_v(row)) << 4); }
+  // Of rows `row` + lane / kChunks: bytes from that row of the memory that lane fetches from
+  static __device__ __forceinline__ unsigned int k_from(int lane, int row, unsigned int stride) {
+    return (unsigned int)(lane / kChunks) * stride + 16u * ((lane % kChunks) ^ swz_k(row + lane / kChunks));
+  }
+  static __device__ __forceinline__ unsigned int v_from(int lane, int row, unsigned int stride) {
+    return (unsigned int)(lane / kChunks) * stride + 16u * ((lane % kChunks) ^ swz_v(row + lane / kChunks));
+  }
 };
 
 // The pages of a request's KV head: where the rows from a token on are.  Rows of one load lie on one page (16 tokens and more).
@@ -75,10 +88,10 @@ __device__ __forceinline__ bf16x4 lds_tr(const unsigned char *p) {
 }
 // Offsets into a tile from which a lane's operands are one XOR (columns) and an immediate (rows) away: K of columns 16 ks .. by k_at ^ ks <<
 // 5, V^T of the 32-wide d-block db by vt_at ^ db << 6.
-template <int kD> __device__ __forceinline__ int k_at(int lane) { return Tile<kD>::at(lane & 31, lane >> 5); }
+template <int kD, bool kFold = true> __device__ __forceinline__ int k_at(int lane) { return Tile<kD, kFold>::k(lane & 31, lane >> 5); }
 template <int kD> __device__ __forceinline__ int vt_at(int lane) {
   const int p = lane & 15;
-  return Tile<kD>::at(4 * (lane >> 5) + (p >> 2), 2 * ((lane >> 4) & 1) + ((p >> 1) & 1)) + 8 * (p & 1);
+  return Tile<kD>::v(4 * (lane >> 5) + (p >> 2), 2 * ((lane >> 4) & 1) + ((p >> 1) & 1)) + 8 * (p & 1);
 }
 // V^T operand of the 16-key step `s`, from the block's offset.  Lane: d 32 db + lane % 32, keys 16 s + 8 jj + 4 h + 0..3.
 template <int kD> __device__ __forceinline__ bf16x8 read_vt(const unsigned char *at, int s) {

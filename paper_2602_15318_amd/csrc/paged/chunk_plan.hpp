@@ -60,7 +60,13 @@ struct Plan {
   int T, n_blocks[kMaxPerLane], n_splits[kMaxPerLane], end[kMaxPerLane];
   Request rq[kMaxPerLane];
 };
-__device__ __forceinline__ int splits_of(int L, int T) { return quotient(max(L - 1, 0), T, __builtin_amdgcn_rcpf((float)T)) + 1; }
+// Pieces of a request's blocks.  In blocks of 256 rows and heads of 128, a request whose rows leave half of the wavefronts idle gets pieces of
+// twice the length: a tile of its takes half as long (chunk of 512 beside 16 single tokens, contexts of up to 8,192 tokens: 130 -> 110
+// us; with heads of 64 the softmax of one wavefront sets the pace either way, 82 -> 97).
+template <int kBM> __device__ __forceinline__ int splits_of(const ChunkArgs &a, const Request &r, int T) {
+  if (kBM == 256 && a.d == 128 && r.n <= kBM / 2 / a.g) T *= 2;
+  return quotient(max(r.L - 1, 0), T, __builtin_amdgcn_rcpf((float)T)) + 1;
+}
 // Lane l's requests l, l + 64, ...
 template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a, int lane) {
   Plan p;
@@ -81,14 +87,14 @@ template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a,
   }
   const int U = lane_value(wave_scan(blocks), 63);
   const float W = wave_sum_valu(weight);
-  p.T = 1 << 30;
+  p.T = 1 << 29;
   int best = 1 << 30;
   for (int round = 1; round * a.round <= a.slots; ++round) {
     const int N = round * a.round;
     if (N <= U) continue;
     // T1 = W / (N - U) always fits; the smallest that does lies between W / N and it, and is looked for where they differ by much.
     // (the factor: the sum is off by 2^-16 at most)
-    const auto grains = [&](float t) { return (min((int)(t * (1.f + 0x1p-14f)), 1 << 29) + kGrain) / kGrain; };
+    const auto grains = [&](float t) { return (min((int)(t * (1.f + 0x1p-14f)), 1 << 28) + kGrain) / kGrain; };
     int hi = grains(W / (float)(N - U));
     if (N < 8 * U) {
       int lo = max(grains(W / (float)N) - 1, 0);             // (lo: too small, or not tried)
@@ -97,12 +103,12 @@ template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a,
         int sum = 0;
 #pragma unroll
         for (int k = 0; k < kMaxPerLane; ++k)
-          if (64 * k < a.B) sum += min(p.n_blocks[k], a.slots) * splits_of(p.rq[k].L, mid * kGrain);
+          if (64 * k < a.B) sum += min(p.n_blocks[k], a.slots) * splits_of<kBM>(a, p.rq[k], mid * kGrain);
         if (lane_value(wave_scan(sum), 63) <= N) hi = mid;
         else lo = mid;
       }
     }
-    const int cost = round * (hi + 4);                       // (a piece's beginning and end take as long as four grains)
+    const int cost = round * (hi + (kBM == 256 ? 2 : 4));    // (so many grains a piece's beginning and end take)
     if (cost < best) {
       best = cost;
       p.T = hi * kGrain;
@@ -114,7 +120,7 @@ template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a,
     p.n_splits[k] = 1;
     p.end[k] = before;
     if (64 * k < a.B) {
-      p.n_splits[k] = splits_of(p.rq[k].L, p.T);
+      p.n_splits[k] = splits_of<kBM>(a, p.rq[k], p.T);
       p.end[k] = before + wave_scan(p.n_blocks[k] * p.n_splits[k]);
       before = lane_value(p.end[k], 63);
     }

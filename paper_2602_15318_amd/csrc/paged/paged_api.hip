@@ -218,7 +218,7 @@ int sparrow_chunk_attn(const sparrow_paged_desc *desc, const void *q, const void
   a.table_stride = table_stride; a.q_row = desc->q_stride_row;
   a.stride_page = desc->kv_stride_page; a.stride_token = desc->kv_stride_token; a.stride_head = desc->kv_stride_head;
   a.B = B; a.n_rows = n_rows; a.max_new = max_new; a.Hq = desc->n_q_heads; a.Hkv = desc->n_kv_heads;
-  a.g = desc->n_q_heads / desc->n_kv_heads;
+  a.g = desc->n_q_heads / desc->n_kv_heads; a.d = desc->head_dim;
   a.table_width = table_width; a.page_shift = shift_of(desc->page_size); a.n_pages = desc->n_pages;
   a.scale_log2 = (desc->scale > 0.f ? desc->scale : 1.0f / std::sqrt((float)desc->head_dim)) * kLog2e;
   a.inv_g = 1.0f / (float)a.g;
