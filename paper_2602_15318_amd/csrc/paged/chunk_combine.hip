@@ -1,19 +1,26 @@
-// Second pass of the chunk attention: the pieces of a block's keys put together.  kSpread wavefronts (16, 4, or 1: the more rows, the
-// fewer) share the pieces of one (row of the batch, query head), all loads of a wavefront on their way at once.
+// Second pass of the chunk attention: the pieces of a block's keys put together.  kD / 4 lanes take a row's piece, 16 bytes each; the groups of
+// kSpread wavefronts (8 or 2) share the pieces of one (row of the batch, query head), the loads of up to 8 pieces of a group on their
+// way at once.  Where there are many rows (kSpread 1), each group takes a head of its own.
 #include "chunk_plan.hpp"
 
 namespace sparrow {
 
 namespace {
 
-constexpr int kAtOnce = 8;
+struct State { float top, l; f32x4 o; };
+__device__ __forceinline__ void add(State &s, float m, float l, f32x4 o) {
+  const float t = fmaxf(s.top, m), f = fast_exp2(s.top - t), g = fast_exp2(m - t);
+  s.l = fmaf(s.l, f, l * g);
+  s.o = s.o * f + o * g;
+  s.top = t;
+}
 
 template <typename T, int kD, int kBM, int kSpread>
 __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combine_kernel(ChunkArgs a) {
-  constexpr int kWaves = kSpread == 1 ? 4 : kSpread;
-  constexpr int kPer = kD / 64;                            // floats of a lane
-  __shared__ float sum_o[kWaves][kD], sum_l[kWaves], tops[kWaves];
-  const int lane = threadIdx.x & 63;
+  constexpr int kGroup = kD / 4, kGroups = 64 / kGroup, kAtOnce = kSpread == 1 ? 4 : 8, kParts = kSpread * kGroups;
+  __shared__ __attribute__((aligned(16))) float sum_o[kParts][kD];
+  __shared__ float sum_ml[kParts][2];
+  const int lane = threadIdx.x & 63, group = lane / kGroup, at4 = 4 * (lane % kGroup);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.y + 32768 * blockIdx.z;
   if (r >= a.n_rows) return;
@@ -35,73 +42,54 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combi
       }
     }
   if (b < 0 || n_splits == 1) return;                      // (in one piece: written already)
+  if (first < 0 || first + n_blocks * n_splits > a.slots) return;      // (offsets that overlap promise any number of pieces)
   const int i = r - q.row0;
-  const int part = kSpread > 1 ? w : 0;                    // which of the row's pieces
-  for (int h = kSpread > 1 ? (int)blockIdx.x : w; h < a.Hq; h += kSpread > 1 ? (int)gridDim.x : kWaves) {
-    const int c = quotient(h, a.g), rho = i * a.g + h - c * a.g, block = rho / kBM;
-    const int piece0 = first + n_blocks - 1 - block;
-    if (piece0 < 0 || piece0 + (n_splits - 1) * n_blocks >= a.slots) return;     // (offsets that overlap promise any number of pieces)
-    const auto at = [&](int s) { return ((int64_t)(piece0 + s * n_blocks) * a.Hkv + c) * kBM + rho % kBM; };
-    float top = kNegBig, l = 0.f, o[kPer];
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) o[e] = 0.f;
-    for (int s0 = part; s0 < n_splits; s0 += kSpread * kAtOnce) {
-      float m[kAtOnce], ls[kAtOnce], x[kAtOnce][kPer];
+  const bool none = q.past + i < 0;
+  const int part = w * kGroups + group;                    // kSpread 1: the head; else which of the pieces
+  for (int h = kSpread > 1 ? (int)blockIdx.x : part; h < a.Hq; h += kSpread > 1 ? a.Hq : 4 * kGroups) {
+    const int c = quotient(h, a.g, a.inv_g), rho = i * a.g + h - c * a.g;
+    const int64_t at0 = ((int64_t)(first + n_blocks - 1 - rho / kBM) * a.Hkv + c) * kBM + rho % kBM;
+    const auto at = [&](int s) { return at0 + (int64_t)s * n_blocks * a.Hkv * kBM; };
+    State st{kNegBig, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    constexpr int kStep = kSpread > 1 ? kParts : 1;
+    for (int s0 = kSpread > 1 ? part : 0; s0 < n_splits; s0 += kStep * kAtOnce) {
+      float m[kAtOnce], l[kAtOnce];
+      f32x4 o[kAtOnce];
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
-        const int64_t k = at(min(s0 + kSpread * u, n_splits - 1));
+        const int64_t k = at(min(s0 + kStep * u, n_splits - 1));
         m[u] = a.part_ml[2 * k];
-        ls[u] = a.part_ml[2 * k + 1];
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) x[u][e] = a.part_o[k * kD + kPer * lane + e];
+        l[u] = a.part_ml[2 * k + 1];
+        o[u] = *(const f32x4 *)(a.part_o + k * kD + at4);
       }
-      float t = top;
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        if (s0 + kSpread * u >= n_splits) m[u] = kNegBig, ls[u] = 0.f;
-        t = fmaxf(t, m[u]);
-      }
-      const float f0 = fast_exp2(top - t);
-      l *= f0;
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) o[e] *= f0;
-#pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        if (s0 + kSpread * u >= n_splits) continue;
-        const float f = fast_exp2(m[u] - t);
-        l = fmaf(ls[u], f, l);
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) o[e] = fmaf(x[u][e], f, o[e]);
-      }
-      top = t;
+      for (int u = 0; u < kAtOnce; ++u)
+        if (s0 + kStep * u < n_splits) add(st, m[u], l[u], o[u]);
     }
     if constexpr (kSpread > 1) {
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) sum_o[w][kPer * lane + e] = o[e];
-      if (lane == 0) { sum_l[w] = l; tops[w] = top; }
+      *(f32x4 *)&sum_o[part][at4] = st.o;
+      if (at4 == 0) { sum_ml[part][0] = st.top; sum_ml[part][1] = st.l; }
       __syncthreads();
-      if (w != 0) return;
-      float t = tops[0], ls = 0.f;
-#pragma unroll
-      for (int k = 1; k < kWaves; ++k) t = fmaxf(t, tops[k]);
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) o[e] = 0.f;
-#pragma unroll
-      for (int k = 0; k < kWaves; ++k) {
-        const float f = fast_exp2(tops[k] - t);
-        ls = fmaf(sum_l[k], f, ls);
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) o[e] = fmaf(sum_o[k][kPer * lane + e], f, o[e]);
+      if (part != 0) return;
+      const int n = min(kParts, n_splits);                 // those that had a piece
+      for (int k = 1; k < n; ++k) st.top = fmaxf(st.top, sum_ml[k][0]);
+      st.l = 0.f;
+      st.o = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+      for (int k = 0; k < n; ++k) {
+        const float f = fast_exp2(sum_ml[k][0] - st.top);
+        st.l = fmaf(sum_ml[k][1], f, st.l);
+        st.o += *(const f32x4 *)&sum_o[k][at4] * f;
       }
-      l = ls;
-      top = t;
     }
-    const bool none = q.past + i < 0;
     const int64_t to = (int64_t)r * a.Hq + h;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) Elem<T>::store((T *)a.out + to * kD + kPer * lane + e, none ? 0.f : o[e] / l);
-    if (a.lse && lane == 0) a.lse[to] = none ? -INFINITY : (top + fast_log2(l)) * kLn2;
-    if (kSpread > 1) return;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    if (!none) x = st.o / st.l;
+    if constexpr (sizeof(T) == 4)
+      *(f32x4 *)((float *)a.out + to * kD + at4) = x;
+    else
+      *(u32x2 *)((bf16_t *)a.out + to * kD + at4) = (u32x2){pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+    if (a.lse && at4 == 0) a.lse[to] = none ? -INFINITY : (st.top + fast_log2(st.l)) * kLn2;
   }
 }
 
@@ -109,8 +97,8 @@ template <typename T, int kD, int kBM> hipError_t launch(const ChunkArgs &a, hip
   const int y = a.n_rows < 32768 ? a.n_rows : 32768, z = (a.n_rows + 32767) / 32768;
   // as many wavefronts a (row, head) as the chip holds
   const int64_t rows = (int64_t)a.n_rows * a.Hq;
-  if (rows <= 512) hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, 16>), dim3(a.Hq, y, z), dim3(1024), 0, st, a);
-  else if (rows <= 2048) hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, 4>), dim3(a.Hq, y, z), dim3(256), 0, st, a);
+  if (rows <= 1024) hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, 8>), dim3(a.Hq, y, z), dim3(512), 0, st, a);
+  else if (rows <= 4096) hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, 2>), dim3(a.Hq, y, z), dim3(128), 0, st, a);
   else hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, 1>), dim3(1, y, z), dim3(256), 0, st, a);
   return hipGetLastError();
 }
