@@ -15,13 +15,17 @@ ChunkShape chunk_shape(int dtype, int d, int Hq, int Hkv, int B, int64_t n_rows,
   ChunkShape s;
   const int64_t rows = std::min<int64_t>(max_new, n_rows) * (Hq / Hkv);        // of a request, at most
   const bool f32 = dtype == SPARROW_F32;
-  s.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : f32 || rows <= 64 ? 64 : 256;
+  #ifndef R32
+#define R32 64
+#endif
+  s.rows = rows <= 16 ? 16 : f32 ? (rows <= 32 ? 32 : 64) : rows <= 32 ? 32 : rows <= 64 ? 64 : 256;
   // every request ends in a block of its own, not all of it filled
   s.blocks = rows <= s.rows ? B : (int)(n_rows * (Hq / Hkv) / s.rows) + B;
+  const int each = (int)std::min<int64_t>((rows + s.rows - 1) / s.rows, 8);
   // workgroups that run at once
   const int at_once = s.rows == 256 ? 256 : s.rows == 16 && !f32 ? 512 : f32 && s.rows == 64 ? (d == 128 ? 512 : 1024) : 256;
-  if (rows <= s.rows) {
-    s.round = std::max(at_once / Hkv, 2 * B);
+  if (s.rows < 256 && !(f32 && rows > s.rows)) {
+    s.round = std::max(at_once / Hkv, 2 * B * each);
     // Requests of up to 256 tokens, bf16, in one piece each and without a second pass: one token over 250 tokens 9.3 -> 7.2 us, over 500 9.6 -> 11.
     s.slots = capacity <= 256 && !f32 ? 0 : s.round;
   } else {

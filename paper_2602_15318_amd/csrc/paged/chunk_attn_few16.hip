@@ -91,7 +91,8 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few16_kernel(ChunkArgs a) {
       for (int g = 0; g < kG; ++g) q[rt][g] = ((const u32x4 *)at)[4 * g + c4];
     }
     wait_loads<0>();
-    for (int it = 0; it < n; ++it) {
+    auto step = [&](int it, auto masked) __attribute__((always_inline)) {
+      constexpr bool kMasked = decltype(masked)::value;
       const int buf = it & 1;
       const bool more = it + 1 < n, more2 = it + 2 < n;
       if (more) wait_loads<3 * kLoads>();
@@ -118,11 +119,10 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few16_kernel(ChunkArgs a) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more2) issue(Kg, true, w + (it + 2) * kWaves, 2 * buf);
       const int t = pc.t0 + (w + it * kWaves) * kTokens;
-      const bool edge = t + kTokens - 1 > min(first_pos, t1 - 1);          // some row does not see all of the tile
       float p[kRT][4], seen[kRT][4];
 #pragma unroll
       for (int rt = 0; rt < kRT; ++rt) {
-        if (edge) {
+        if constexpr (kMasked) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const bool vis = t + 4 * c4 + i <= min(pos[rt], t1 - 1);
@@ -146,43 +146,43 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few16_kernel(ChunkArgs a) {
       if (more2) wait_loads<3 * kLoads>();
       else if (more) wait_loads<2 * kLoads>();
       else wait_loads<0>();
-      auto output = [&](auto masked) __attribute__((always_inline)) {
-        constexpr bool kMasked = decltype(masked)::value;
-        if constexpr (kF32) {
+      if constexpr (kF32) {
 #pragma unroll
-          for (int db = 0; db < kDB; ++db)
+        for (int db = 0; db < kDB; ++db)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float v = *reinterpret_cast<const float *>(V + (4 * c4 + i) * kRow + (16 * db + n16) * 4);
+          for (int i = 0; i < 4; ++i) {
+            const float v = *reinterpret_cast<const float *>(V + (4 * c4 + i) * kRow + (16 * db + n16) * 4);
 #pragma unroll
-              for (int rt = 0; rt < kRT; ++rt)
-                o[rt][db] = kMasked ? add_masked4(v, p[rt][i], seen[rt][i], o[rt][db])
-                                    : __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[rt][i], o[rt][db], 0, 0, 0);
-            }
-        } else {
-          // probabilities are rounded to bf16 for the product (their sum is not): 2^-9 of a term on average, of the result less
-          bf16x4 pb[kRT], ones[kRT];
-#pragma unroll
-          for (int rt = 0; rt < kRT; ++rt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              pb[rt][i] = (__bf16)p[rt][i];
-              if (kMasked) ones[rt][i] = (__bf16)seen[rt][i];
-            }
-          const int row = 4 * c4 + (n16 >> 2);
-#pragma unroll
-          for (int db = 0; db < kDB; ++db) {
-            const bf16x4 v = lds_tr(V + row * kRow + (((2 * db + ((n16 >> 1) & 1)) ^ swz(row)) << 4) + 8 * (n16 & 1));
-#pragma unroll
-            for (int rt = 0; rt < kRT; ++rt) o[rt][db] = kMasked ? add_masked16(v, pb[rt], ones[rt], o[rt][db]) : mul16(v, pb[rt], o[rt][db]);
+            for (int rt = 0; rt < kRT; ++rt)
+              o[rt][db] = kMasked ? add_masked4(v, p[rt][i], seen[rt][i], o[rt][db])
+                                  : __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[rt][i], o[rt][db], 0, 0, 0);
           }
+      } else {
+        // probabilities are rounded to bf16 for the product (their sum is not): 2^-9 of a term on average, of the result less
+        bf16x4 pb[kRT], ones[kRT];
+#pragma unroll
+        for (int rt = 0; rt < kRT; ++rt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            pb[rt][i] = (__bf16)p[rt][i];
+            if (kMasked) ones[rt][i] = (__bf16)seen[rt][i];
+          }
+        const int row = 4 * c4 + (n16 >> 2);
+#pragma unroll
+        for (int db = 0; db < kDB; ++db) {
+          const bf16x4 v = lds_tr(V + row * kRow + (((2 * db + ((n16 >> 1) & 1)) ^ swz(row)) << 4) + 8 * (n16 & 1));
+#pragma unroll
+          for (int rt = 0; rt < kRT; ++rt) o[rt][db] = kMasked ? add_masked16(v, pb[rt], ones[rt], o[rt][db]) : mul16(v, pb[rt], o[rt][db]);
         }
-      };
-      if (edge) output(std::true_type());
-      else output(std::false_type());
+      }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more2) issue(Vg, !kF32, w + (it + 2) * kWaves, 2 * buf + 1);
-    }
+    };
+    // the tiles that all rows of the block see whole, then the others
+    const int full = max(min(first_pos + 1, t1) - pc.t0, 0) / kTokens, n_full = max(full - w + kWaves - 1, 0) / kWaves;
+    int it = 0;
+    for (; it < n_full; ++it) step(it, std::false_type());
+    for (; it < n; ++it) step(it, std::true_type());
   }
   // ---- merge: states of the wavefronts through LDS
   __syncthreads();

@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
   Piece pc;
   if (!find_piece<kBM>(a, idx, lane, &pc)) return;         // uniform
   const Pages pages = pages_of(a, pc, c);
-  const int R = pc.rq.n * a.g;
+  const int rho0 = pc.block * kBM, R = pc.rq.n * a.g - rho0;      // rows of the request from the block's first on
 
   unsigned char *mine = lds + w * 4 * kTileBytes;
   const unsigned int mine_at = lds_offset(mine);
@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
   int pos[kRT];
 #pragma unroll
   for (int rt = 0; rt < kRT; ++rt) {
-    const int rho = min(32 * rt + (lane & 31), R - 1);
+    const int rho = rho0 + min(32 * rt + (lane & 31), R - 1);
     pos[rt] = min(pc.rq.past + (int)(((float)rho + 0.5f) * a.inv_g), pc.rq.L - 1);
   }
   f32x16 o[kRT][kDB];
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
     constexpr int kQLoads = kRT * kLoads;
 #pragma unroll
     for (int j = 0; j < kQLoads; ++j) {
-      const int rho = min(j * Rows::kLoadRows + lane / Rows::kChunks, R - 1);
+      const int rho = rho0 + min(j * Rows::kLoadRows + lane / Rows::kChunks, R - 1);
       const int i = (int)(((float)rho + 0.5f) * a.inv_g);
       const unsigned char *at = (const unsigned char *)a.q + 2 * ((int64_t)(pc.rq.row0 + i) * a.q_row + (int64_t)(c * a.g + rho - i * a.g) * kD);
       const int row = j * Rows::kLoadRows + lane / Rows::kChunks;
@@ -90,7 +90,8 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
       issue(false, w + kWaves, 2);
       issue(true, w + kWaves, 3);
     }
-    for (int it = 0; it < n; ++it) {
+    auto step = [&](int it, auto masked) __attribute__((always_inline)) {
+      constexpr bool kMasked = decltype(masked)::value;
       const int buf = it & 1;
       const bool more = it + 1 < n, more2 = it + 2 < n;
       if (more) wait_loads<3 * kLoads>();
@@ -108,11 +109,10 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more2) issue(false, w + (it + 2) * kWaves, 2 * buf);
       const int t = pc.t0 + (w + it * kWaves) * kTokens;
-      const bool edge = t + kTokens - 1 > min(pc.rq.past, pc.t1 - 1);     // some row does not see all of the tile
       bf16x8 pb[kRT][2], seen[kRT][2];
 #pragma unroll
       for (int rt = 0; rt < kRT; ++rt) {
-        if (edge) {
+        if constexpr (kMasked) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int key = t + 8 * (e >> 2) + 4 * h + (e & 3);
@@ -144,23 +144,25 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
       if (more2) wait_loads<3 * kLoads>();
       else if (more) wait_loads<2 * kLoads>();
       else wait_loads<0>();
-      auto output = [&](auto masked) __attribute__((always_inline)) {
 #pragma unroll
-        for (int db = 0; db < kDB; ++db)
+      for (int db = 0; db < kDB; ++db)
 #pragma unroll
-          for (int st = 0; st < 2; ++st) {
-            const bf16x8 v = read_vt<kD>(V + (vt_at<kD>(lane) ^ db << 6), st);
+        for (int st = 0; st < 2; ++st) {
+          const bf16x8 v = read_vt<kD>(V + (vt_at<kD>(lane) ^ db << 6), st);
 #pragma unroll
-            for (int rt = 0; rt < kRT; ++rt)
-              o[rt][db] = decltype(masked)::value ? add_masked(v, pb[rt][st], seen[rt][st], o[rt][db])
-                                                  : __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[rt][st], o[rt][db], 0, 0, 0);
-          }
-      };
-      if (edge) output(std::true_type());
-      else output(std::false_type());
+          for (int rt = 0; rt < kRT; ++rt)
+            o[rt][db] = kMasked ? add_masked(v, pb[rt][st], seen[rt][st], o[rt][db])
+                                                : __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[rt][st], o[rt][db], 0, 0, 0);
+        }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more2) issue(true, w + (it + 2) * kWaves, 2 * buf + 1);
-    }
+    };
+    // the tiles that all rows of the block see whole, then the others
+    const int first_pos = pc.rq.past + quotient(rho0, a.g);
+    const int full = max(min(first_pos + 1, pc.t1) - pc.t0, 0) / kTokens, n_full = max(full - w + kWaves - 1, 0) / kWaves;
+    int it = 0;
+    for (; it < n_full; ++it) step(it, std::false_type());
+    for (; it < n; ++it) step(it, std::true_type());
   }
   // ---- merge: states of the four wavefronts, fp32, through LDS
   __syncthreads();
@@ -183,7 +185,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
   const bool direct = pc.n_splits == 1;
   if (!direct && idx >= a.slots) return;                   // (offsets that overlap)
   const int64_t part = ((int64_t)idx * a.Hkv + c) * kBM;
-  for (int x = threadIdx.x; x < R * kRowChunks; x += 64 * kWaves) {
+  for (int x = threadIdx.x; x < min(R, kBM) * kRowChunks; x += 64 * kWaves) {
     const int r = x / kRowChunks, chunk = x % kRowChunks;
     float top = ml[0][r][0];
 #pragma unroll
@@ -204,8 +206,8 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
       }
       continue;
     }
-    const int i = (int)(((float)r + 0.5f) * a.inv_g);
-    const int64_t at = (int64_t)(pc.rq.row0 + i) * a.Hq + c * a.g + r - i * a.g;
+    const int rho = rho0 + r, i = (int)(((float)rho + 0.5f) * a.inv_g);
+    const int64_t at = (int64_t)(pc.rq.row0 + i) * a.Hq + c * a.g + rho - i * a.g;
     const bool none = pc.rq.past + i < 0;
     const float inv = 1.f / ls;
     if (none) sum = (f32x4){0.f, 0.f, 0.f, 0.f};
