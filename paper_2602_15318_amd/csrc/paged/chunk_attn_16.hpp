@@ -26,24 +26,43 @@ __device__ __forceinline__ f32x4 infinities(f32x4 o, f32x4 up, f32x4 down) {
   for (int i = 0; i < 4; ++i) o[i] += (up[i] > 0.f ? INFINITY : 0.f) + (down[i] > 0.f ? -INFINITY : 0.f);
   return o;
 }
-// As add_masked (chunk_attn_mfma.hpp): a product of a tile in which some rows do not see some keys.
-__device__ __forceinline__ f32x4 add_masked16(bf16x4 v, bf16x4 p, bf16x4 seen, f32x4 o) {
-  u32x2 w = __builtin_bit_cast(u32x2, v);
-  const u32x2 bad = {no_numbers(w[0]), no_numbers(w[1])};
-  if (__builtin_amdgcn_ballot_w64((bad[0] | bad[1]) != 0u) == 0ull) return mul16(v, p, o);
+// As add_masked (chunk_attn_mfma.hpp), of 16 keys.
+template <int kN> __device__ __forceinline__ void add_masked16(const bf16x4 (&v)[kN], bf16x4 p, bf16x4 seen, f32x4 *o) {
+  unsigned int any = 0u;
+#pragma unroll
+  for (int db = 0; db < kN; ++db) any |= not_finite(__builtin_bit_cast(u32x2, v[db])[0]) | not_finite(__builtin_bit_cast(u32x2, v[db])[1]);
+  if (__builtin_amdgcn_ballot_w64(any != 0u) == 0ull) {
+#pragma unroll
+    for (int db = 0; db < kN; ++db) o[db] = mul16(v[db], p, o[db]);
+    return;
+  }
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  const u32x2 up = {ones_of(w[0], false), ones_of(w[1], false)}, down = {ones_of(w[0], true), ones_of(w[1], true)};
-  w &= ~bad;
-  return infinities(mul16(__builtin_bit_cast(bf16x4, w), p, o), mul16(__builtin_bit_cast(bf16x4, up), seen, zero),
-                    mul16(__builtin_bit_cast(bf16x4, down), seen, zero));
+#pragma unroll
+  for (int db = 0; db < kN; ++db) {
+    const u32x2 w = __builtin_bit_cast(u32x2, v[db]), fine = {w[0] & ~no_numbers(w[0]), w[1] & ~no_numbers(w[1])};
+    const u32x2 up = {ones_of(w[0], false), ones_of(w[1], false)}, down = {ones_of(w[0], true), ones_of(w[1], true)};
+    o[db] = infinities(mul16(__builtin_bit_cast(bf16x4, fine), p, o[db]), mul16(__builtin_bit_cast(bf16x4, up), seen, zero),
+                       mul16(__builtin_bit_cast(bf16x4, down), seen, zero));
+  }
 }
-__device__ __forceinline__ f32x4 add_masked4(float v, float p, float seen, f32x4 o) {
-  const bool no = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u, nan = v != v;
-  if (__builtin_amdgcn_ballot_w64(no) == 0ull) return __builtin_amdgcn_mfma_f32_16x16x4f32(v, p, o, 0, 0, 0);
+// Of one k-step of the fp32 product, 4 keys.
+template <int kN> __device__ __forceinline__ void add_masked4(const float (&v)[kN], float p, float seen, f32x4 *o) {
+  bool any = false;
+#pragma unroll
+  for (int db = 0; db < kN; ++db) any |= (__float_as_uint(v[db]) & 0x7f800000u) == 0x7f800000u;
+  if (__builtin_amdgcn_ballot_w64(any) == 0ull) {
+#pragma unroll
+    for (int db = 0; db < kN; ++db) o[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[db], p, o[db], 0, 0, 0);
+    return;
+  }
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  return infinities(__builtin_amdgcn_mfma_f32_16x16x4f32(no ? 0.f : v, p, o, 0, 0, 0),
-                    __builtin_amdgcn_mfma_f32_16x16x4f32(nan || (no && v > 0.f) ? 1.f : 0.f, seen, zero, 0, 0, 0),
-                    __builtin_amdgcn_mfma_f32_16x16x4f32(nan || (no && v < 0.f) ? 1.f : 0.f, seen, zero, 0, 0, 0));
+#pragma unroll
+  for (int db = 0; db < kN; ++db) {
+    const bool no = (__float_as_uint(v[db]) & 0x7f800000u) == 0x7f800000u, nan = v[db] != v[db];
+    o[db] = infinities(__builtin_amdgcn_mfma_f32_16x16x4f32(no ? 0.f : v[db], p, o[db], 0, 0, 0),
+                       __builtin_amdgcn_mfma_f32_16x16x4f32(nan || (no && v[db] > 0.f) ? 1.f : 0.f, seen, zero, 0, 0, 0),
+                       __builtin_amdgcn_mfma_f32_16x16x4f32(nan || (no && v[db] < 0.f) ? 1.f : 0.f, seen, zero, 0, 0, 0));
+  }
 }
 
 }  // namespace sparrow

@@ -65,11 +65,12 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_f32_kernel(ChunkArgs a) 
       for (int g = 0; g < kG; ++g) q[g] = ((const f32x4 *)at)[4 * g + c4];
     }
     const bool have = rho0 + 16 * w < R;                   // the wavefront has rows
-    for (int t = 0; t < n; ++t) {
+    auto step = [&](int t, auto masked) __attribute__((always_inline)) {
+      constexpr bool kMasked = decltype(masked)::value;
       wait_loads<0>();
       barrier();                                           // tile t is there, and nobody reads tile t - 1
       if (t + 1 < n) issue(t + 1, (t + 1) & 1);
-      if (!have) continue;
+      if (!have) return;
       const unsigned char *K = lds + 2 * (t & 1) * kTileBytes, *V = K + kTileBytes;
       f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
@@ -82,9 +83,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_f32_kernel(ChunkArgs a) 
           for (int j = 0; j < 2; ++j) s[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j][i], q[g][i], s[j], 0, 0, 0);
       }
       const int t0 = pc.t0 + t * kTokens;
-      const bool edge = t0 + kTokens - 1 > min(first_pos, t1 - 1);         // some row does not see all of the tile
       float p[2][4], seen[2][4];
-      if (edge) {
+      if constexpr (kMasked) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -111,20 +111,26 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_f32_kernel(ChunkArgs a) 
         for (int i = 0; i < 4; ++i) p[j][i] = fast_exp2(fmaf(s[j][i], a.scale_log2, -m));
         l += (p[j][0] + p[j][1]) + (p[j][2] + p[j][3]);
       }
-      auto output = [&](auto masked) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+          float v[kDB];
 #pragma unroll
-            for (int db = 0; db < kDB; ++db) {
-              const float v = *reinterpret_cast<const float *>(V + j * kSlab + (4 * c4 + i) * kRow + (16 * db + n16) * 4);
-              o[db] = decltype(masked)::value ? add_masked4(v, p[j][i], seen[j][i], o[db]) : __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[j][i], o[db], 0, 0, 0);
-            }
-      };
-      if (edge) output(std::true_type());
-      else output(std::false_type());
-    }
+          for (int db = 0; db < kDB; ++db) v[db] = *reinterpret_cast<const float *>(V + j * kSlab + (4 * c4 + i) * kRow + (16 * db + n16) * 4);
+          if constexpr (kMasked) {
+            add_masked4(v, p[j][i], seen[j][i], o);
+          } else {
+#pragma unroll
+            for (int db = 0; db < kDB; ++db) o[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[db], p[j][i], o[db], 0, 0, 0);
+          }
+        }
+    };
+    // the tiles that all rows of the block see whole, then the others
+    const int n_full = min(n, max(min(first_pos + 1, t1) - pc.t0, 0) / kTokens);
+    int t = 0;
+    for (; t < n_full; ++t) step(t, std::false_type());
+    for (; t < n; ++t) step(t, std::true_type());
   }
   // ---- the block's rows, or its partial of this piece: elements 16 db + 4 c4 + 0..3 of a row
   l = quad_sum(l);

@@ -148,31 +148,40 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few16_kernel(ChunkArgs a) {
       else wait_loads<0>();
       if constexpr (kF32) {
 #pragma unroll
-        for (int db = 0; db < kDB; ++db)
+        for (int i = 0; i < 4; ++i) {
+          float v[kDB];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float v = *reinterpret_cast<const float *>(V + (4 * c4 + i) * kRow + (16 * db + n16) * 4);
+          for (int db = 0; db < kDB; ++db) v[db] = *reinterpret_cast<const float *>(V + (4 * c4 + i) * kRow + (16 * db + n16) * 4);
 #pragma unroll
-            for (int rt = 0; rt < kRT; ++rt)
-              o[rt][db] = kMasked ? add_masked4(v, p[rt][i], seen[rt][i], o[rt][db])
-                                  : __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[rt][i], o[rt][db], 0, 0, 0);
+          for (int rt = 0; rt < kRT; ++rt) {
+            if constexpr (kMasked) {
+              add_masked4(v, p[rt][i], seen[rt][i], o[rt]);
+            } else {
+#pragma unroll
+              for (int db = 0; db < kDB; ++db) o[rt][db] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[db], p[rt][i], o[rt][db], 0, 0, 0);
+            }
           }
+        }
       } else {
         // probabilities are rounded to bf16 for the product (their sum is not): 2^-9 of a term on average, of the result less
-        bf16x4 pb[kRT], ones[kRT];
+        const int row = 4 * c4 + (n16 >> 2);
+        bf16x4 v[kDB];
 #pragma unroll
-        for (int rt = 0; rt < kRT; ++rt)
+        for (int db = 0; db < kDB; ++db) v[db] = lds_tr(V + row * kRow + (((2 * db + ((n16 >> 1) & 1)) ^ swz(row)) << 4) + 8 * (n16 & 1));
+#pragma unroll
+        for (int rt = 0; rt < kRT; ++rt) {
+          bf16x4 pb, ones;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            pb[rt][i] = (__bf16)p[rt][i];
-            if (kMasked) ones[rt][i] = (__bf16)seen[rt][i];
+            pb[i] = (__bf16)p[rt][i];
+            if (kMasked) ones[i] = (__bf16)seen[rt][i];
           }
-        const int row = 4 * c4 + (n16 >> 2);
+          if constexpr (kMasked) {
+            add_masked16(v, pb, ones, o[rt]);
+          } else {
 #pragma unroll
-        for (int db = 0; db < kDB; ++db) {
-          const bf16x4 v = lds_tr(V + row * kRow + (((2 * db + ((n16 >> 1) & 1)) ^ swz(row)) << 4) + 8 * (n16 & 1));
-#pragma unroll
-          for (int rt = 0; rt < kRT; ++rt) o[rt][db] = kMasked ? add_masked16(v, pb[rt], ones[rt], o[rt][db]) : mul16(v, pb[rt], o[rt][db]);
+            for (int db = 0; db < kDB; ++db) o[rt][db] = mul16(v[db], pb, o[rt][db]);
+          }
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

@@ -145,15 +145,20 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
       else if (more) wait_loads<2 * kLoads>();
       else wait_loads<0>();
 #pragma unroll
-      for (int db = 0; db < kDB; ++db)
+      for (int st = 0; st < 2; ++st) {
+        bf16x8 v[kDB];
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          const bf16x8 v = read_vt<kD>(V + (vt_at<kD>(lane) ^ db << 6), st);
+        for (int db = 0; db < kDB; ++db) v[db] = read_vt<kD>(V + (vt_at<kD>(lane) ^ db << 6), st);
 #pragma unroll
-          for (int rt = 0; rt < kRT; ++rt)
-            o[rt][db] = kMasked ? add_masked(v, pb[rt][st], seen[rt][st], o[rt][db])
-                                                : __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[rt][st], o[rt][db], 0, 0, 0);
+        for (int rt = 0; rt < kRT; ++rt) {
+          if constexpr (kMasked) {
+            add_masked(v, pb[rt][st], seen[rt][st], o[rt]);
+          } else {
+#pragma unroll
+            for (int db = 0; db < kDB; ++db) o[rt][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[db], pb[rt][st], o[rt][db], 0, 0, 0);
+          }
         }
+      }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more2) issue(true, w + (it + 2) * kWaves, 2 * buf + 1);
     };

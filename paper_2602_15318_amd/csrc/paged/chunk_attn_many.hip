@@ -223,11 +223,11 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_many_kernel(ChunkArgs a)
           bf16x8 ones;
 #pragma unroll
           for (int e = 0; e < 8; ++e) ones[e] = (__bf16)(16 * st + 8 * (e >> 2) + (e & 3) <= seen ? 1.f : 0.f);
+          bf16x8 v[kDB];
 #pragma unroll
-          for (int db = 0; db < kDB; ++db) {
-            o[db] = add_masked(read_vt<kD>(lds + (vt ^ db << 6), st), pb[st], ones, o[db]);
-            __builtin_amdgcn_sched_barrier(0);
-          }
+          for (int db = 0; db < kDB; ++db) v[db] = read_vt<kD>(lds + (vt ^ db << 6), st);
+          add_masked(v, pb[st], ones, o);
+          __builtin_amdgcn_sched_barrier(0);
         }
         read_k(tile(t + 1, 0, k0), 0, kf);
         wait_loads<2 * kLoads>();

@@ -108,10 +108,9 @@ __device__ __forceinline__ float pair_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Elements of an operand that are no numbers: bit masks of their halves.
-__device__ __forceinline__ unsigned int no_numbers(unsigned int w) {
-  return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
-}
+// Two bf16 elements: the top bit of each half that is no number, and the whole halves.
+__device__ __forceinline__ unsigned int not_finite(unsigned int w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ unsigned int no_numbers(unsigned int w) { return (not_finite(w) >> 15) * 0xffffu; }
 // 1.0 in the halves that are infinite of that sign, or NaN
 __device__ __forceinline__ unsigned int ones_of(unsigned int w, bool negative) {
   unsigned int r = 0u;
@@ -123,29 +122,37 @@ __device__ __forceinline__ unsigned int ones_of(unsigned int w, bool negative) {
   }
   return r;
 }
-// O^T += V^T P^T of one operand of a tile in which some rows do not see some keys.  0 * inf must not reach those rows, so what is no number
-// leaves the operand; whether a row sees one such value or more is counted by products of ones, exactly, and adds the infinities then (a NaN
-// counts as both).
-__device__ __forceinline__ f32x16 add_masked(bf16x8 v, bf16x8 p, bf16x8 seen, f32x16 o) {
-  u32x4 w = __builtin_bit_cast(u32x4, v), bad;
+// O^T += V^T P^T of a 16-key step of a tile in which some rows do not see some keys, all d-blocks.  0 * inf must not reach those rows, so what is
+// no number leaves the operand; whether a row sees one such value or more is counted by products of ones, exactly, and adds the infinities
+// then (a NaN counts as both).
+template <int kN> __device__ __forceinline__ void add_masked(const bf16x8 (&v)[kN], bf16x8 p, bf16x8 seen, f32x16 *o) {
+  unsigned int any = 0u;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) bad[i] = no_numbers(w[i]);
-  const bool any = (bad[0] | bad[1] | bad[2] | bad[3]) != 0u;
-  if (__builtin_amdgcn_ballot_w64(any) == 0ull) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, o, 0, 0, 0);
-  u32x4 up, down;
+  for (int db = 0; db < kN; ++db)
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    up[i] = ones_of(w[i], false);
-    down[i] = ones_of(w[i], true);
-    w[i] &= ~bad[i];
+    for (int i = 0; i < 4; ++i) any |= not_finite(__builtin_bit_cast(u32x4, v[db])[i]);
+  if (__builtin_amdgcn_ballot_w64(any != 0u) == 0ull) {
+#pragma unroll
+    for (int db = 0; db < kN; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[db], p, o[db], 0, 0, 0);
+    return;
   }
-  o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p, o, 0, 0, 0);
-  const f32x16 zero = {0.f};
-  const f32x16 cu = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, up), seen, zero, 0, 0, 0);
-  const f32x16 cd = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, down), seen, zero, 0, 0, 0);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) o[e] += (cu[e] > 0.f ? INFINITY : 0.f) + (cd[e] > 0.f ? -INFINITY : 0.f);
-  return o;
+  for (int db = 0; db < kN; ++db) {
+    u32x4 w = __builtin_bit_cast(u32x4, v[db]), up, down;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      up[i] = ones_of(w[i], false);
+      down[i] = ones_of(w[i], true);
+      w[i] &= ~no_numbers(w[i]);
+    }
+    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p, o[db], 0, 0, 0);
+    const f32x16 zero = {0.f};
+    const f32x16 cu = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, up), seen, zero, 0, 0, 0);
+    const f32x16 cd = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, down), seen, zero, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[db][e] += (cu[e] > 0.f ? INFINITY : 0.f) + (cd[e] > 0.f ? -INFINITY : 0.f);
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 
 }  // namespace sparrow
