@@ -159,6 +159,14 @@ PyObject *tuple(std::initializer_list<at::Tensor> items) {      // an undefined 
   return Py_NewRef(r.get());
 }
 
+// The part of a one-dimensional tensor from `first` on: an allocation of its own costs the host more.
+at::Tensor part(const at::Tensor &whole, int64_t first, int64_t n) {
+  at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
+  t.unsafeGetTensorImpl()->set_storage_offset(first);
+  t.unsafeGetTensorImpl()->set_sizes_contiguous({n});
+  return t;
+}
+
 struct Table { int32_t *at; int32_t width; int64_t stride; };
 Table table(Call &c, PyObject *o, int64_t B) {
   const at::Tensor &t = c.tensor(o);
@@ -214,7 +222,12 @@ PyObject *page_update(PyObject *const *a) {
   at::Tensor out[4];
   const int64_t sizes[4] = {n, B + 1, n, 1};
   if (none(a[8])) {
-    for (int i = 0; i < 4; ++i) out[i] = at::empty({sizes[i]}, old.options());
+    const at::Tensor whole = at::empty({sizes[0] + sizes[1] + sizes[2] + sizes[3]}, old.options());
+    int64_t first = 0;
+    for (int i = 0; i < 4; ++i) {
+      out[i] = part(whole, first, sizes[i]);
+      first += sizes[i];
+    }
   } else {
     need(PyTuple_CheckExact(a[8]) && PyTuple_GET_SIZE(a[8]) == 4);
     for (int i = 0; i < 4; ++i) {

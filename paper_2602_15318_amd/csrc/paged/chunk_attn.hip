@@ -5,7 +5,7 @@
 
 namespace sparrow {
 
-hipError_t launch_chunk_few16(int dtype, int d, int rows, int blocks, const ChunkArgs &a, hipStream_t st);
+hipError_t launch_chunk_few16(int dtype, int d, int rows, int waves, int blocks, const ChunkArgs &a, hipStream_t st);
 hipError_t launch_chunk_few32(int d, int rows, int blocks, const ChunkArgs &a, hipStream_t st);
 hipError_t launch_chunk_f32(int d, int blocks, const ChunkArgs &a, hipStream_t st);
 hipError_t launch_chunk_many(int d, int blocks, const ChunkArgs &a, hipStream_t st);
@@ -15,17 +15,17 @@ ChunkShape chunk_shape(int dtype, int d, int Hq, int Hkv, int B, int64_t n_rows,
   ChunkShape s;
   const int64_t rows = std::min<int64_t>(max_new, n_rows) * (Hq / Hkv);        // of a request, at most
   const bool f32 = dtype == SPARROW_F32;
-  #ifndef R32
-#define R32 64
-#endif
-  s.rows = rows <= 16 ? 16 : f32 ? (rows <= 32 ? 32 : 64) : rows <= 32 ? 32 : rows <= 64 ? 64 : 256;
+  s.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : f32 || rows <= 64 ? 64 : 256;
   // every request ends in a block of its own, not all of it filled
   s.blocks = rows <= s.rows ? B : (int)(n_rows * (Hq / Hkv) / s.rows) + B;
-  const int each = (int)std::min<int64_t>((rows + s.rows - 1) / s.rows, 8);
+  // Single tokens: the fewer (request, KV head) pairs, the fewer and larger the workgroups, and the fewer pieces there are to put together.  us with 8
+  // / 4 / 2 wavefronts, 256 / 512 / 1,024 workgroups at once, 28/4 heads of 128: one request of 26,112 tokens 15.9 / 16.8 / 18.9, eight of up to 8,000
+  // 19.6 / 20.4 / 22.1, 32 of up to 4,000 32.4 / 31.3 / 32.5, 96 of up to 3,000 68.4 / 70.5 / 65.7, 200 of up to 2,048 104 / 95 / 91.
+  s.waves = f32 ? 4 : B * Hkv <= 48 ? 8 : B * Hkv < 192 ? 4 : 2;
   // workgroups that run at once
-  const int at_once = s.rows == 256 ? 256 : s.rows == 16 && !f32 ? 512 : f32 && s.rows == 64 ? (d == 128 ? 512 : 1024) : 256;
-  if (s.rows < 256 && !(f32 && rows > s.rows)) {
-    s.round = std::max(at_once / Hkv, 2 * B * each);
+  const int at_once = s.rows == 16 && !f32 ? 2048 / s.waves : f32 && s.rows == 64 ? (d == 128 ? 512 : 1024) : 256;
+  if (rows <= s.rows) {
+    s.round = std::max(at_once / Hkv, 2 * B);
     // Requests of up to 256 tokens, bf16, in one piece each and without a second pass: one token over 250 tokens 9.3 -> 7.2 us, over 500 9.6 -> 11.
     s.slots = capacity <= 256 && !f32 ? 0 : s.round;
   } else {
@@ -44,7 +44,7 @@ hipError_t launch_chunk_attn(int dtype, int d, const ChunkArgs &a, hipStream_t s
   const ChunkShape s = chunk_shape(dtype, d, a.Hq, a.Hkv, a.B, a.n_rows, a.max_new, (int64_t)a.table_width << a.page_shift);
   const int blocks = std::max(s.blocks, s.slots);
   hipError_t e;
-  if (s.rows == 16 || (dtype == SPARROW_F32 && s.rows == 32)) e = launch_chunk_few16(dtype, d, s.rows, blocks, a, st);
+  if (s.rows == 16 || (dtype == SPARROW_F32 && s.rows == 32)) e = launch_chunk_few16(dtype, d, s.rows, s.waves, blocks, a, st);
   else if (dtype == SPARROW_F32) e = launch_chunk_f32(d, blocks, a, st);
   else if (s.rows < 256) e = launch_chunk_few32(d, s.rows, blocks, a, st);
   else e = launch_chunk_many(d, blocks, a, st);

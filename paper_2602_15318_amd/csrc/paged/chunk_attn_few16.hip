@@ -252,11 +252,11 @@ template <typename T, int kRT, int kWaves> hipError_t launch(int d, dim3 grid, c
 
 }  // namespace
 
-hipError_t launch_chunk_few16(int dtype, int d, int rows, int blocks, const ChunkArgs &a, hipStream_t st) {
+hipError_t launch_chunk_few16(int dtype, int d, int rows, int waves, int blocks, const ChunkArgs &a, hipStream_t st) {
   const dim3 grid(a.Hkv, blocks < 32768 ? blocks : 32768, (blocks + 32767) / 32768);
   if (dtype == SPARROW_F32)
     return rows == 16 ? launch<float, 1, 4>(d, grid, a, st) : launch<float, 2, 4>(d, grid, a, st);
-  return launch<bf16_t, 1, 4>(d, grid, a, st);
+  return waves == 8 ? launch<bf16_t, 1, 8>(d, grid, a, st) : waves == 2 ? launch<bf16_t, 1, 2>(d, grid, a, st) : launch<bf16_t, 1, 4>(d, grid, a, st);
 }
 
 }  // namespace sparrow

@@ -49,9 +49,10 @@ struct ChunkArgs {
   float scale_log2, inv_g;
   float *part_o, *part_ml; // [piece * Hkv + KV head][row of the block]: unnormalised output [d]; reference point (log2), sum
 };
-// How a call of these sizes is run: rows per block, blocks of the batch at most, pieces per KV head, floats of part_o and part_ml.
+// How a call of these sizes is run: rows per block, blocks per KV head at most, pieces, wavefronts per workgroup
+// (blocks of 16 rows), floats of part_o and part_ml.
 struct ChunkShape {
-  int rows, blocks, slots, round;
+  int rows, blocks, slots, round, waves;
   int64_t floats_o, floats_ml;
 };
 ChunkShape chunk_shape(int dtype, int d, int Hq, int Hkv, int B, int64_t n_rows, int max_new, int64_t capacity);
