@@ -9,7 +9,7 @@ hipError_t launch_chunk_few16(int dtype, int d, int rows, int waves, int blocks,
 hipError_t launch_chunk_few32(int d, int rows, int blocks, const ChunkArgs &a, hipStream_t st);
 hipError_t launch_chunk_f32(int d, int blocks, const ChunkArgs &a, hipStream_t st);
 hipError_t launch_chunk_many(int d, int blocks, const ChunkArgs &a, hipStream_t st);
-hipError_t launch_chunk_combine(int dtype, int d, int rows, const ChunkArgs &a, hipStream_t st);
+hipError_t launch_chunk_combine(int dtype, int d, const ChunkArgs &a, hipStream_t st);
 
 ChunkShape chunk_shape(int dtype, int d, int Hq, int Hkv, int B, int64_t n_rows, int max_new, int64_t capacity) {
   ChunkShape s;
@@ -49,7 +49,7 @@ hipError_t launch_chunk_attn(int dtype, int d, const ChunkArgs &a, hipStream_t s
   else if (s.rows < 256) e = launch_chunk_few32(d, s.rows, blocks, a, st);
   else e = launch_chunk_many(d, blocks, a, st);
   if (e != hipSuccess || s.slots == 0) return e;
-  return launch_chunk_combine(dtype, d, s.rows, a, st);
+  return launch_chunk_combine(dtype, d, a, st);
 }
 
 }  // namespace sparrow

@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_f32_kernel(ChunkArgs a) 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = blockIdx.x, idx = blockIdx.y + 32768 * blockIdx.z;
   Piece pc;
-  if (!find_piece<kBM>(a, idx, lane, &pc)) return;         // uniform
+  if (!find_piece(a, idx, lane, &pc)) return;         // uniform
   const int R = pc.rq.n * a.g, rho0 = pc.block * kBM;
   const auto table = (const int32_t __attribute__((address_space(4))) *)(uintptr_t)(a.block_table + (int64_t)pc.b * a.table_stride);
   const unsigned char *Kg = (const unsigned char *)((const float *)a.k + c * a.stride_head);

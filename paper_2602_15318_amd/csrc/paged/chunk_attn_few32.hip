@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = blockIdx.x, idx = blockIdx.y;
   Piece pc;
-  if (!find_piece<kBM>(a, idx, lane, &pc)) return;         // uniform
+  if (!find_piece(a, idx, lane, &pc)) return;         // uniform
   const Pages pages = pages_of(a, pc, c);
   const int rho0 = pc.block * kBM, R = pc.rq.n * a.g - rho0;      // rows of the request from the block's first on
 

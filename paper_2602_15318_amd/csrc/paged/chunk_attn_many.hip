@@ -25,7 +25,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_many_kernel(ChunkArgs a)
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = blockIdx.x, idx = blockIdx.y + 32768 * blockIdx.z;
   Piece pc;
-  if (!find_piece<kBM>(a, idx, lane, &pc)) return;         // uniform
+  if (!find_piece(a, idx, lane, &pc)) return;         // uniform
   const Pages pages = pages_of(a, pc, c);
   const int R = pc.rq.n * a.g, rho0 = pc.block * kBM;
   const bool have = rho0 + 32 * w < R;                     // the wavefront has rows

@@ -15,7 +15,7 @@ __device__ __forceinline__ void add(State &s, float m, float l, f32x4 o) {
   s.top = t;
 }
 
-template <typename T, int kD, int kBM, int kSpread>
+template <typename T, int kD, int kSpread>
 __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combine_kernel(ChunkArgs a) {
   constexpr int kGroup = kD / 4, kGroups = 64 / kGroup, kAtOnce = kSpread == 1 ? 4 : 8, kParts = kSpread * kGroups;
   __shared__ __attribute__((aligned(16))) float sum_o[kParts][kD];
@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combi
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.y + 32768 * blockIdx.z;
   if (r >= a.n_rows) return;
-  const Plan p = make_plan<kBM>(a, lane);
+  const Plan p = make_plan(a, lane);
   int b = -1, n_blocks = 0, n_splits = 0, first = 0;
   Request q{};
 #pragma unroll
@@ -48,8 +48,8 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combi
   const int part = w * kGroups + group;                    // kSpread 1: the head; else which of the pieces
   for (int h = kSpread > 1 ? (int)blockIdx.x : part; h < a.Hq; h += kSpread > 1 ? a.Hq : 4 * kGroups) {
     const int c = quotient(h, a.g, a.inv_g), rho = i * a.g + h - c * a.g;
-    const int64_t at0 = ((int64_t)(first + n_blocks - 1 - rho / kBM) * a.Hkv + c) * kBM + rho % kBM;
-    const auto at = [&](int s) { return at0 + (int64_t)s * n_blocks * a.Hkv * kBM; };
+    const int64_t at0 = (((int64_t)(first + n_blocks - 1 - (rho >> a.block_shift)) * a.Hkv + c) << a.block_shift) + (rho & ((1 << a.block_shift) - 1));
+    const auto at = [&](int s) { return at0 + ((int64_t)s * n_blocks * a.Hkv << a.block_shift); };
     State st{kNegBig, 0.f, {0.f, 0.f, 0.f, 0.f}};
     constexpr int kStep = kSpread > 1 ? kParts : 1;
     for (int s0 = kSpread > 1 ? part : 0; s0 < n_splits; s0 += kStep * kAtOnce) {
@@ -93,28 +93,21 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combi
   }
 }
 
-template <typename T, int kD, int kBM> hipError_t launch(const ChunkArgs &a, hipStream_t st) {
+template <typename T, int kD> hipError_t launch(const ChunkArgs &a, hipStream_t st) {
   const int y = a.n_rows < 32768 ? a.n_rows : 32768, z = (a.n_rows + 32767) / 32768;
   // as many wavefronts a (row, head) as the chip holds
   const int64_t rows = (int64_t)a.n_rows * a.Hq;
-  if (rows <= 1024) hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, 8>), dim3(a.Hq, y, z), dim3(512), 0, st, a);
-  else if (rows <= 4096) hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, 2>), dim3(a.Hq, y, z), dim3(128), 0, st, a);
-  else hipLaunchKernelGGL((chunk_combine_kernel<T, kD, kBM, 1>), dim3(1, y, z), dim3(256), 0, st, a);
+  if (rows <= 1024) hipLaunchKernelGGL((chunk_combine_kernel<T, kD, 8>), dim3(a.Hq, y, z), dim3(512), 0, st, a);
+  else if (rows <= 4096) hipLaunchKernelGGL((chunk_combine_kernel<T, kD, 2>), dim3(a.Hq, y, z), dim3(128), 0, st, a);
+  else hipLaunchKernelGGL((chunk_combine_kernel<T, kD, 1>), dim3(1, y, z), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_chunk_combine(int dtype, int d, int rows, const ChunkArgs &a, hipStream_t st) {
-  const bool f32 = dtype == SPARROW_F32;
-#define SPARROW_ROWS(n) \
-  if (rows == n && f32) return d == 128 ? launch<float, 128, n>(a, st) : launch<float, 64, n>(a, st); \
-  if (rows == n) return d == 128 ? launch<bf16_t, 128, n>(a, st) : launch<bf16_t, 64, n>(a, st);
-  SPARROW_ROWS(16)
-  SPARROW_ROWS(32)
-  SPARROW_ROWS(64)
-#undef SPARROW_ROWS
-  return d == 128 ? launch<bf16_t, 128, 256>(a, st) : launch<bf16_t, 64, 256>(a, st);
+hipError_t launch_chunk_combine(int dtype, int d, const ChunkArgs &a, hipStream_t st) {
+  if (dtype == SPARROW_F32) return d == 128 ? launch<float, 128>(a, st) : launch<float, 64>(a, st);
+  return d == 128 ? launch<bf16_t, 128>(a, st) : launch<bf16_t, 64>(a, st);
 }
 
 }  // namespace sparrow

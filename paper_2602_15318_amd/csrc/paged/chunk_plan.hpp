@@ -1,7 +1,7 @@
 // Which piece of the batch a workgroup of the chunk attention takes.  Lengths live on the device, so the workgroups work the
 // plan out themselves, each the same one: a wavefront holds a request per lane (and register, above 64 requests).
 //
-// A row is a (new token, query head of the group) pair; the rows of a request and KV head are cut into blocks of kBM rows, a
+// A row is a (new token, query head of the group) pair; the rows of a request and KV head are cut into blocks, a
 // block's keys into pieces of T tokens at most, T as small as it may be for the sum over the blocks of ceil(length / T) to be at
 // most N, the pieces per KV head that the chip holds at once, or twice that if two rounds of shorter pieces end sooner.  Blocks are not cut
 // at all where N is not above their number U.
@@ -63,12 +63,12 @@ struct Plan {
 // Pieces of a request's blocks.  In blocks of 256 rows and heads of 128, a request whose rows leave half of the wavefronts idle gets pieces of
 // twice the length: a tile of its takes half as long (chunk of 512 beside 16 single tokens, contexts of up to 8,192 tokens: 130 -> 110
 // us; with heads of 64 the softmax of one wavefront sets the pace either way, 82 -> 97).
-template <int kBM> __device__ __forceinline__ int splits_of(const ChunkArgs &a, const Request &r, int T) {
-  if (kBM == 256 && a.d == 128 && r.n <= kBM / 2 / a.g) T *= 2;
+__device__ __forceinline__ int splits_of(const ChunkArgs &a, const Request &r, int T) {
+  if (a.block_shift == 8 && a.d == 128 && r.n <= 128 / a.g) T *= 2;
   return quotient(max(r.L - 1, 0), T, __builtin_amdgcn_rcpf((float)T)) + 1;
 }
 // Lane l's requests l, l + 64, ...
-template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a, int lane) {
+__device__ __forceinline__ Plan make_plan(const ChunkArgs &a, int lane) {
   Plan p;
   int blocks = 0;
   float weight = 0.f;
@@ -79,7 +79,7 @@ template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a,
     if (64 * k < a.B) {
       if (64 * k + lane < a.B) {
         p.rq[k] = request_of(a, 64 * k + lane);
-        p.n_blocks[k] = (int)(((int64_t)p.rq[k].n * a.g + kBM - 1) / kBM);
+        p.n_blocks[k] = (int)(((int64_t)p.rq[k].n * a.g + (1 << a.block_shift) - 1) >> a.block_shift);
       }
       blocks += min(p.n_blocks[k], a.slots);               // (offsets that overlap may promise any number)
       weight += (float)p.n_blocks[k] * (float)p.rq[k].L;
@@ -103,12 +103,12 @@ template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a,
         int sum = 0;
 #pragma unroll
         for (int k = 0; k < kMaxPerLane; ++k)
-          if (64 * k < a.B) sum += min(p.n_blocks[k], a.slots) * splits_of<kBM>(a, p.rq[k], mid * kGrain);
+          if (64 * k < a.B) sum += min(p.n_blocks[k], a.slots) * splits_of(a, p.rq[k], mid * kGrain);
         if (lane_value(wave_scan(sum), 63) <= N) hi = mid;
         else lo = mid;
       }
     }
-    const int cost = round * (hi + (kBM == 256 ? 2 : 4));    // (so many grains a piece's beginning and end take)
+    const int cost = round * (hi + (a.block_shift == 8 ? 2 : 4));    // (so many grains a piece's beginning and end take)
     if (cost < best) {
       best = cost;
       p.T = hi * kGrain;
@@ -120,7 +120,7 @@ template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a,
     p.n_splits[k] = 1;
     p.end[k] = before;
     if (64 * k < a.B) {
-      p.n_splits[k] = splits_of<kBM>(a, p.rq[k], p.T);
+      p.n_splits[k] = splits_of(a, p.rq[k], p.T);
       p.end[k] = before + wave_scan(p.n_blocks[k] * p.n_splits[k]);
       before = lane_value(p.end[k], 63);
     }
@@ -129,8 +129,8 @@ template <int kBM> __device__ __forceinline__ Plan make_plan(const ChunkArgs &a,
 }
 
 // Piece number `idx` of a KV head; false: there are not that many.  Blocks count down: the last, whose rows see most, come first.
-template <int kBM> __device__ __forceinline__ bool find_piece(const ChunkArgs &a, int idx, int lane, Piece *out) {
-  const Plan p = make_plan<kBM>(a, lane);
+__device__ __forceinline__ bool find_piece(const ChunkArgs &a, int idx, int lane, Piece *out) {
+  const Plan p = make_plan(a, lane);
   Piece q;
   q.b = -1;
   int end = 0;

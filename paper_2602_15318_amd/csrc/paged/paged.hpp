@@ -45,6 +45,7 @@ struct ChunkArgs {
   float *lse;
   int64_t table_stride, q_row, stride_page, stride_token, stride_head;          // elements
   int32_t B, n_rows, max_new, Hq, Hkv, g, d, table_width, page_shift, n_pages;
+  int32_t block_shift;     // log2 of the rows of a block
   int32_t slots, round;    // pieces per KV head that the blocks of rows may be cut into (0: one piece each); those that run at once
   float scale_log2, inv_g;
   float *part_o, *part_ml; // [piece * Hkv + KV head][row of the block]: unnormalised output [d]; reference point (log2), sum

@@ -223,7 +223,7 @@ int sparrow_chunk_attn(const sparrow_paged_desc *desc, const void *q, const void
   a.scale_log2 = (desc->scale > 0.f ? desc->scale : 1.0f / std::sqrt((float)desc->head_dim)) * kLog2e;
   a.inv_g = 1.0f / (float)a.g;
   const ChunkShape shape = chunk_shape(desc->dtype, desc->head_dim, a.Hq, a.Hkv, B, n_rows, max_new, (int64_t)table_width * desc->page_size);
-  a.slots = shape.slots; a.round = shape.round;
+  a.slots = shape.slots; a.round = shape.round; a.block_shift = shift_of(shape.rows);
   a.part_o = (float *)workspace;
   a.part_ml = (float *)((unsigned char *)workspace + round_up((size_t)shape.floats_o * 4, 256));
   const hipError_t e = launch_chunk_attn(desc->dtype, desc->head_dim, a, (hipStream_t)hip_stream);

@@ -155,20 +155,20 @@ class _Call:
     """The device and stream of a call: `with _Call(device, stream, tensors allocated here) as handle`."""
 
     def __init__(self, device, stream, *made):
-        current = torch.cuda.current_device()
-        self.back = None if device.index == current else current
-        if self.back is not None:
-            torch.cuda.set_device(device)
-        raw = torch._C._cuda_getCurrentRawStream(device.index)
-        if stream is not None and stream.cuda_stream != raw:
-            raw = stream.cuda_stream
-            for t in made:                  # freed, it may be handed out again only once that stream has passed
-                if t is not None:
-                    t.record_stream(stream)
-        self.handle = raw
+        self.device, self.stream, self.made = device, stream, made
 
     def __enter__(self):
-        return self.handle
+        current = torch.cuda.current_device()
+        self.back = None if self.device.index == current else current
+        raw = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if self.stream is not None and self.stream.cuda_stream != raw:
+            raw = self.stream.cuda_stream
+            for t in self.made:             # freed, it may be handed out again only once that stream has passed
+                if t is not None:
+                    t.record_stream(self.stream)
+        if self.back is not None:
+            torch.cuda.set_device(self.device)
+        return raw
 
     def __exit__(self, *_):
         if self.back is not None:

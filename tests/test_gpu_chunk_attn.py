@@ -146,6 +146,19 @@ def test_rows_of_a_fused_product_and_wide_tables(sp, dtype):
     check(sp, x)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B", [1, 7, 30, 130])
+def test_pieces_put_together(sp, dtype, d, B):
+    """Batches of few and many rows, single tokens and a few, whose requests are all cut: each has its share of a second pass's wavefronts."""
+    kv = [2000 - 13 * b for b in range(B)]
+    check(sp, ref.Batch(kv, [1] * B, dtype, 16, 4, d, 16, seed=B, width=200), "single tokens")
+    if B < 100:
+        new = [1 + b % 5 for b in range(B)]
+        check(sp, ref.Batch(kv, new, dtype, 40, 4, d, 64, seed=B, width=200), "up to five tokens, 50 rows a KV head")
+        check(sp, ref.Batch(kv, [n + 4 for n in new], dtype, 8, 1, d, 64, "head", seed=B), "up to nine tokens, 72 rows")
+
+
 def test_two_hundred_and_fifty_six_requests(sp):
     g = torch.Generator().manual_seed(1)
     kv = torch.randint(1, 700, (256,), generator=g).tolist()
