@@ -58,8 +58,9 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combi
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
         const int64_t k = at(min(s0 + kStep * u, n_splits - 1));
-        m[u] = a.part_ml[2 * k];
-        l[u] = a.part_ml[2 * k + 1];
+        const float2 ml = ((const float2 *)a.part_ml)[k];
+        m[u] = ml.x;
+        l[u] = ml.y;
         o[u] = *(const f32x4 *)(a.part_o + k * kD + at4);
       }
 #pragma unroll
