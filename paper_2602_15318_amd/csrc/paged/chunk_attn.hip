@@ -26,8 +26,9 @@ ChunkShape chunk_shape(int dtype, int d, int Hq, int Hkv, int B, int64_t n_rows,
   const int at_once = s.rows == 16 && !f32 ? 2048 / s.waves : f32 && s.rows == 64 ? (d == 128 ? 512 : 1024) : 256;
   if (rows <= s.rows) {
     s.round = std::max(at_once / Hkv, 2 * B);
-    // Requests of up to 256 tokens, bf16, in one piece each and without a second pass: one token over 250 tokens 9.3 -> 7.2 us, over 500 9.6 -> 11.
-    s.slots = capacity <= 256 && !f32 ? 0 : s.round;
+    // Requests of up to 512 tokens (fp32: 128, a tile takes three times as long) in one piece each and without a second pass, us: one token of 28/4
+    // heads over 380 tokens 9.3 -> 6.9, over 500 9.4 -> 7.5, over 1,000 10.6 -> 10.1, four such 11.0 -> 14.0; fp32 over 120 10.5 -> 8.1, over 250 10.5 -> 11.5.
+    s.slots = capacity <= (f32 ? 128 : 512) ? 0 : s.round;
   } else {
     // cut only where that fills the chip better; two rounds of pieces if they end sooner
     const int64_t filled = (n_rows * (Hq / Hkv) + s.rows - 1) / s.rows;
