@@ -33,7 +33,7 @@ typedef struct {
   int32_t n_q_heads;    /* Hq */
   int32_t n_kv_heads;   /* Hkv, divides Hq */
   int32_t head_dim;     /* d: 64 or 128 */
-  float scale;          /* softmax scale; 0 selects 1/sqrt(head_dim); read by sparrow_chunk_attn only */
+  float scale;          /* softmax scale; 0 selects 1/sqrt(head_dim); up to 2.3e38; read by sparrow_chunk_attn only */
   int32_t page_size;    /* tokens per page: a power of two from 16 to 4096 */
   int32_t n_pages;      /* pages of the cache; n_pages * page_size < 2^31 */
   /* Element (page p, token t of it, head c, 0) of a cache, K and V alike: p*kv_stride_page + t*kv_stride_token +

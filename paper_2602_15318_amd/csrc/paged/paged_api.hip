@@ -64,8 +64,8 @@ int check_desc(const sparrow_paged_desc *d) {
                   "head_dim to 2^40 elements", (long long)st[0], (long long)st[1], (long long)st[2]);
   if ((int64_t)d->page_size * d->kv_stride_token * es >= 1ll << 31)
     return fail(SPARROW_ERR_UNSUPPORTED, "page_size * kv_stride_token: tokens of a page more than 2^31 bytes apart");
-  if (!(d->scale >= 0.f) || std::isinf(d->scale))
-    return fail(SPARROW_ERR_INVALID_ARG, "scale must be finite and >= 0 (0 = 1/sqrt(head_dim))");
+  if (!(d->scale >= 0.f) || std::isinf(d->scale * kLog2e))      // (scores are kept in base 2)
+    return fail(SPARROW_ERR_INVALID_ARG, "scale must be >= 0 (0 = 1/sqrt(head_dim)), and finite in base 2: up to 2.3e38");
   return SPARROW_OK;
 }
 

@@ -54,7 +54,7 @@ BAD_DESC = [(dict(dtype=2), UNSUPPORTED), (dict(n_q_heads=30), INVALID), (dict(n
             (dict(n_pages=0), INVALID), (dict(n_pages=1 << 27), UNSUPPORTED), (dict(kv_stride_head=132), INVALID),
             (dict(kv_stride_token=64), INVALID), (dict(kv_stride_page=0), INVALID), (dict(kv_stride_token=1 << 27), UNSUPPORTED),
             (dict(kv_stride_page=1 << 41), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
-            (dict(scale=float("inf")), INVALID), (dict(q_stride_row=27 * 128), INVALID), (dict(q_stride_row=28 * 128 + 4), INVALID)]
+            (dict(scale=float("inf")), INVALID), (dict(scale=2.5e38), INVALID), (dict(q_stride_row=27 * 128), INVALID), (dict(q_stride_row=28 * 128 + 4), INVALID)]
 
 
 def _chunk(p, desc, q=P, k=P, v=P, table=P, width=10, stride=10, cu=P, kv=P, B=2, rows=5, max_new=3, out=P, lse=P, ws=P, nbytes=1 << 40):
