@@ -1,5 +1,6 @@
 // Attention of chunks of new tokens over the paged cache, fp32: blocks of 64 rows (new token, query head of the group) per request and KV head, products on
-// the matrix cores in fp32 (v_mfma_f32_16x16x4_f32).  Bound by them: 157 TFLOP/s.
+// the matrix cores in fp32 (v_mfma_f32_16x16x4_f32).  Bound by them: 1,000 tokens over 6,000, 28/4 heads
+// of 128, 730 us, 108 TFLOP/s (a library's product of 8,192^3 152).
 //
 // A workgroup of four wavefronts takes one block and piece of keys; wavefront w has rows 16 w .. 16 w + 15.  K and V tiles of 32 keys go memory -> LDS
 // past the registers, one tile ahead; two workgroups share a compute unit, so that one's softmax runs beside the other's products.

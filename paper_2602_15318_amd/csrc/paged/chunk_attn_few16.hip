@@ -1,5 +1,7 @@
 // Attention of few new tokens over the paged cache by 16-row tiles: up to 16 rows (new token, query head of the group) per request and KV head, in
-// fp32 up to 32.  Bound by memory.
+// fp32 up to 32.  Bound by memory: 28/4 heads of 128, 48 single tokens over up to 8,192 (405 MB) 69 us, 5.9 TB/s; one over 26,112 (53.5 MB) 11, 4.9
+// TB/s with launch, plan and first tile in it; the second pass takes 5 to 6.5 more.  16-row tiles against 32-row ones for up to 16 rows: 79 / 83 and
+// 17.3 / 18.1 us a call; for 28 rows over 26,112 tokens 27 / 18, so that more rows take 32-row tiles (chunk_attn_few32.hip).
 //
 // A workgroup takes one block and piece of keys; its wavefronts take the 16-token tiles in turn and know nothing of each other until the
 // end, where their states of a row are merged through LDS.  A tile lies on one page; it travels memory -> LDS past the registers, two

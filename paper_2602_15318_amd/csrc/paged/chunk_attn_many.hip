@@ -4,7 +4,13 @@
 //
 // A workgroup of eight wavefronts takes one block and piece of keys; wavefront w has rows 32 w .. 32 w + 31.  Wavefronts w and w + 4 share
 // a SIMD and run half a step apart: while one is in the products of a step (scores of a tile, output of the tile before), the other is in
-// its softmax.  K and V tiles of 64 keys go memory -> LDS past the registers, four of each, asked for four half steps ahead.
+// its softmax.  K and V tiles of 64 keys go memory -> LDS past the registers, four of each, asked for four to six half steps
+// ahead.  Half a step apart against one barrier a tile: chunk of 2,048 tokens over 26,112, 28/4 heads of 128, 672 / 738 us.
+//
+// Probabilities are rounded to bf16 for the output's product, half a step 2^-9 to 2^-8 of a term; the row's sum takes them unrounded.
+//
+// Measured: that chunk 625 to 690 us by card (1,070 to 1,180 TFLOP/s; matrix cores busy 57 % of the cycles), prompt of 7,001 tokens 325 to 365
+// (960 to 1,080; 53 %), prompt of 6,000 with 32/8 heads of 64 190 to 204.
 #include "chunk_attn_mfma.hpp"
 
 namespace sparrow {
