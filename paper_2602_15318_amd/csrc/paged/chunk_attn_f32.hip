@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_f32_kernel(ChunkArgs a) 
   };
 
   f32x4 o[kDB];
-  float m = kNegBig, l = 0.f;
+  float m = kNothingSeen, l = 0.f;
 #pragma unroll
   for (int db = 0; db < kDB; ++db) o[db] = (f32x4){0.f, 0.f, 0.f, 0.f};
   if (n > 0) {
@@ -98,9 +98,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_f32_kernel(ChunkArgs a) 
       float mx = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
       for (int i = 1; i < 4; ++i) mx = fmaxf(fmaxf(mx, s[0][i]), s[1][i]);
-      mx *= a.scale_log2;
-      if (__builtin_amdgcn_ballot_w64(mx > m + kSlack) != 0ull) {
-        const float m_new = fmaxf(m, quad_max(mx)), alpha = fast_exp2(m - m_new);
+      if (__builtin_amdgcn_ballot_w64((mx - m) * a.scale_log2 > kSlack) != 0ull) {
+        const float m_new = fmaxf(m, quad_max(mx)), alpha = factor(m, m_new, a.scale_log2);
         m = m_new;
         l *= alpha;
 #pragma unroll
@@ -109,7 +108,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_f32_kernel(ChunkArgs a) 
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[j][i] = fast_exp2(fmaf(s[j][i], a.scale_log2, -m));
+        for (int i = 0; i < 4; ++i) p[j][i] = fast_exp2((s[j][i] - m) * a.scale_log2);
         l += (p[j][0] + p[j][1]) + (p[j][2] + p[j][3]);
       }
 #pragma unroll
@@ -145,7 +144,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_f32_kernel(ChunkArgs a) 
       if (!none) x = o[db] / l;
       *reinterpret_cast<f32x4 *>((float *)a.out + to * kD + 16 * db + 4 * c4) = x;
     }
-    if (a.lse && c4 == 0) a.lse[to] = none ? -INFINITY : (m + fast_log2(l)) * kLn2;
+    if (a.lse && c4 == 0) a.lse[to] = none ? -INFINITY : log_sum(m, a.scale_log2, l);
     return;
   }
   if (idx >= a.slots) return;                              // (offsets that overlap)

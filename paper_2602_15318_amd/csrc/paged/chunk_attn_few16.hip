@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few16_kernel(ChunkArgs a) {
     rho[rt] = min(rho0 + 16 * rt + n16, R - 1);
     i_row[rt] = quotient(rho[rt], a.g, a.inv_g);
     pos[rt] = min(pc.rq.past + i_row[rt], pc.rq.L - 1);
-    m[rt] = kNegBig;
+    m[rt] = kNothingSeen;
     l[rt] = 0.f;
 #pragma unroll
     for (int db = 0; db < kDB; ++db) o[rt][db] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -132,17 +132,17 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few16_kernel(ChunkArgs a) {
             seen[rt][i] = vis ? 1.f : 0.f;
           }
         }
-        // the row's reference point moves only when a score of the wavefront's lies more than kSlack above it
-        const float mx = fmaxf(fmaxf(s[rt][0], s[rt][1]), fmaxf(s[rt][2], s[rt][3])) * a.scale_log2;
-        if (__builtin_amdgcn_ballot_w64(mx > m[rt] + kSlack) != 0ull) {
-          const float m_new = fmaxf(m[rt], quad_max(mx)), alpha = fast_exp2(m[rt] - m_new);
+        // the row's reference score moves only when a score of the wavefront's lies more than kSlack above it
+        const float mx = fmaxf(fmaxf(s[rt][0], s[rt][1]), fmaxf(s[rt][2], s[rt][3]));
+        if (__builtin_amdgcn_ballot_w64((mx - m[rt]) * a.scale_log2 > kSlack) != 0ull) {
+          const float m_new = fmaxf(m[rt], quad_max(mx)), alpha = factor(m[rt], m_new, a.scale_log2);
           m[rt] = m_new;
           l[rt] *= alpha;
 #pragma unroll
           for (int db = 0; db < kDB; ++db) o[rt][db] *= alpha;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[rt][i] = fast_exp2(fmaf(s[rt][i], a.scale_log2, -m[rt]));
+        for (int i = 0; i < 4; ++i) p[rt][i] = fast_exp2((s[rt][i] - m[rt]) * a.scale_log2);
         l[rt] += (p[rt][0] + p[rt][1]) + (p[rt][2] + p[rt][3]);
       }
       if (more2) wait_loads<3 * kLoads>();
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few16_kernel(ChunkArgs a) {
     float ls = 0.f;
 #pragma unroll
     for (int k = 0; k < kWaves; ++k) {
-      const float f = fast_exp2(ml[k][r][0] - top);
+      const float f = factor(ml[k][r][0], top, a.scale_log2);
       ls = fmaf(ml[k][r][1], f, ls);
       sum += *reinterpret_cast<const f32x4 *>(lds + k * kBM * kD * 4 + (r * kOut + (chunk ^ (r & 15))) * 16) * f;
     }
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few16_kernel(ChunkArgs a) {
       *reinterpret_cast<f32x4 *>((float *)a.out + at * kD + 4 * chunk) = sum;
     else
       *reinterpret_cast<u32x2 *>((bf16_t *)a.out + at * kD + 4 * chunk) = (u32x2){pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3])};
-    if (a.lse && chunk == 0) a.lse[at] = none ? -INFINITY : (top + fast_log2(ls)) * kLn2;
+    if (a.lse && chunk == 0) a.lse[at] = none ? -INFINITY : log_sum(top, a.scale_log2, ls);
   }
 }
 

@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
   float m[kRT], l[kRT];
 #pragma unroll
   for (int rt = 0; rt < kRT; ++rt) {
-    m[rt] = kNegBig;
+    m[rt] = kNothingSeen;
     l[rt] = 0.f;
 #pragma unroll
     for (int db = 0; db < kDB; ++db) o[rt][db] = (f32x16){0.f};
@@ -125,9 +125,8 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
         float mx = s[rt][0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[rt][e]);
-        mx *= a.scale_log2;
-        if (__builtin_amdgcn_ballot_w64(mx > m[rt] + kSlack) != 0ull) {
-          const float m_new = fmaxf(m[rt], pair_max(mx)), alpha = fast_exp2(m[rt] - m_new);
+        if (__builtin_amdgcn_ballot_w64((mx - m[rt]) * a.scale_log2 > kSlack) != 0ull) {
+          const float m_new = fmaxf(m[rt], pair_max(mx)), alpha = factor(m[rt], m_new, a.scale_log2);
           m[rt] = m_new;
           l[rt] *= alpha;
 #pragma unroll
@@ -136,7 +135,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const float p = fast_exp2(fmaf(s[rt][e], a.scale_log2, -m[rt]));
+          const float p = fast_exp2((s[rt][e] - m[rt]) * a.scale_log2);
           sum += p;
           pb[rt][e >> 3][e & 7] = (__bf16)p;
         }
@@ -200,7 +199,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
     float ls = 0.f;
 #pragma unroll
     for (int k = 0; k < kWaves; ++k) {
-      const float f = fast_exp2(ml[k][r][0] - top);
+      const float f = factor(ml[k][r][0], top, a.scale_log2);
       ls = fmaf(ml[k][r][1], f, ls);
       sum += *reinterpret_cast<const f32x4 *>(lds + k * kBM * kD * 4 + (r * kRowChunks + (chunk ^ (r & (kRowChunks - 1)))) * 16) * f;
     }
@@ -219,7 +218,7 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few32_kernel(ChunkArgs a) {
     if (none) sum = (f32x4){0.f, 0.f, 0.f, 0.f};
     else sum *= inv;
     *reinterpret_cast<u32x2 *>((bf16_t *)a.out + at * kD + 4 * chunk) = (u32x2){pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3])};
-    if (a.lse && chunk == 0) a.lse[at] = none ? -INFINITY : (top + fast_log2(ls)) * kLn2;
+    if (a.lse && chunk == 0) a.lse[at] = none ? -INFINITY : log_sum(top, a.scale_log2, ls);
   }
 }
 

@@ -45,8 +45,17 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_many_kernel(ChunkArgs a)
   // tiles that all rows of the block see whole
   const int n_full = min(n, max(min(t1, pc.rq.past + quotient(rho0, a.g) + 1) - pc.t0, 0) / kTokens);
 
+  // About scaled points r below 2^20 an exponent is one operation, fma(score, scale, -r): the weights are then 2^c of those about m, c what
+  // the rounding of r took off (2^-5 at most), which is taken out where the states leave the workgroup.  Farther points, and a row that has seen
+  // nothing, let every score past their limit and into the branch of the points that move, which takes the difference first.  (Everywhere
+  // the difference first: chunk of 2,048 over 26,112 tokens 651 -> 677 us, prompt of 6,000 with heads of 64 187 -> 205.)
+  const auto far = [&](float r) __attribute__((always_inline)) { return fabsf(r) >= 0x1p20f; };
+  const auto excess = [&](float m) __attribute__((always_inline)) {
+    const float r = m * a.scale_log2;
+    return far(r) ? 0.f : fmaf(m, a.scale_log2, -r);
+  };
   f32x16 o[kDB];
-  float m = kNegBig, l = 0.f;
+  float m = kNothingSeen, r = kNothingSeen, limit = -INFINITY, l = 0.f;
 #pragma unroll
   for (int db = 0; db < kDB; ++db) o[db] = (f32x16){0.f};
   if (n > 0) {
@@ -133,30 +142,32 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_many_kernel(ChunkArgs a)
 #pragma unroll
         for (int st = 0; st < 4; ++st) v[st] = read_vt<kD>(lds + (at ^ db << 6), st);
       };
-      // the scores' exponentials about the row's reference point, which moves only when a score of the wavefront's lies more than
+      // the scores' exponentials about the row's reference score, which moves only when a score of the wavefront's lies more than
       // kSlack above it
       auto softmax = [&]() __attribute__((always_inline)) {
         float x[2][16];
-        auto shift = [&]() __attribute__((always_inline)) {
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[kb][e] = fmaf(s[kb][e], a.scale_log2, -m);
-        };
-        shift();
+          for (int e = 0; e < 16; ++e) x[kb][e] = fmaf(s[kb][e], a.scale_log2, -r);
         float top = fmaxf(x[0][0], x[1][0]);
 #pragma unroll
         for (int e = 1; e < 16; ++e) top = fmaxf(fmaxf(top, x[0][e]), x[1][e]);
-        if (__builtin_amdgcn_ballot_w64(top > kSlack) != 0ull) {
+        if (__builtin_amdgcn_ballot_w64(top > limit) != 0ull) {
           float mx = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
           for (int e = 1; e < 16; ++e) mx = fmaxf(fmaxf(mx, s[0][e]), s[1][e]);
-          const float m_new = fmaxf(m, pair_max(mx * a.scale_log2)), alpha = fast_exp2(m - m_new);
+          const float m_new = fmaxf(m, pair_max(mx)), alpha = fast_exp2(fmaf(m - m_new, a.scale_log2, excess(m_new) - excess(m)));
           m = m_new;
+          r = scaled(m, a.scale_log2);
+          limit = far(r) ? -INFINITY : kSlack;
           l *= alpha;
 #pragma unroll
           for (int db = 0; db < kDB; ++db) o[db] *= alpha;
-          shift();
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[kb][e] = far(r) ? (s[kb][e] - m) * a.scale_log2 : fmaf(s[kb][e], a.scale_log2, -r);
         }
         float sum[2] = {0.f, 0.f};
         u32x4 pw[4];
@@ -247,12 +258,13 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_many_kernel(ChunkArgs a)
     wait_loads<0>();                                       // (no load may land once the workgroup's LDS is another's)
   }
   // ---- the block's rows, or its partial of this piece
-  l = pair_sum(l);
+  const float near = fast_exp2(-excess(m));                // (1 where nothing was seen)
+  l = pair_sum(l) * near;
   if (rho0 + 32 * w + (lane & 31) >= R) return;
   if (pc.n_splits == 1) {
     const bool none = pc.rq.past + i_row < 0;
     const int64_t to = (int64_t)(pc.rq.row0 + i_row) * a.Hq + head;
-    const float inv = none ? 0.f : 1.f / l;
+    const float inv = none ? 0.f : near / l;
 #pragma unroll
     for (int db = 0; db < kDB; ++db)
 #pragma unroll
@@ -262,7 +274,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_many_kernel(ChunkArgs a)
         for (int e = 0; e < 4; ++e) x[e] = none ? 0.f : o[db][4 * j + e] * inv;
         *reinterpret_cast<u32x2 *>((bf16_t *)a.out + to * kD + 32 * db + 8 * j + 4 * h) = (u32x2){pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
       }
-    if (a.lse && h == 0) a.lse[to] = none ? -INFINITY : (m + fast_log2(l)) * kLn2;
+    if (a.lse && h == 0) a.lse[to] = none ? -INFINITY : log_sum(m, a.scale_log2, l);
     return;
   }
   if (idx >= a.slots) return;                              // (offsets that overlap)
@@ -271,7 +283,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) chunk_many_kernel(ChunkArgs a)
   for (int db = 0; db < kDB; ++db)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<f32x4 *>(a.part_o + part * kD + 32 * db + 8 * j + 4 * h) = (f32x4){o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
+      *reinterpret_cast<f32x4 *>(a.part_o + part * kD + 32 * db + 8 * j + 4 * h) = (f32x4){o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]} * near;
   if (h == 0) {
     a.part_ml[2 * part] = m;
     a.part_ml[2 * part + 1] = l;

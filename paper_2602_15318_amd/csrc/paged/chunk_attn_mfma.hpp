@@ -12,8 +12,6 @@ namespace sparrow {
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
-constexpr float kSlack = 8.0f;            // log2 units a score may exceed a row's reference point
-
 // 16 bytes per lane from base + off to LDS, lane l's at dst + 16 l (base and dst uniform).  Not counted by the compiler: wait_loads()
 // waits.  The wait states are those between a scalar register written by the vector ALU, or M0, and its use here.
 template <bool kNt> __device__ __forceinline__ void global_to_lds(const void *base, unsigned int off, unsigned int dst) {

@@ -10,8 +10,8 @@ namespace sparrow {
 namespace {
 
 struct State { float top, l; f32x4 o; };
-__device__ __forceinline__ void add(State &s, float m, float l, f32x4 o) {
-  const float t = fmaxf(s.top, m), f = fast_exp2(s.top - t), g = fast_exp2(m - t);
+__device__ __forceinline__ void add(State &s, float m, float l, f32x4 o, float scale_log2) {
+  const float t = fmaxf(s.top, m), f = factor(s.top, t, scale_log2), g = factor(m, t, scale_log2);
   s.l = fmaf(s.l, f, l * g);
   s.o = s.o * f + o * g;
   s.top = t;
@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combi
     const int c = quotient(h, a.g, a.inv_g), rho = i * a.g + h - c * a.g;
     const int64_t at0 = (((int64_t)(first + n_blocks - 1 - (rho >> a.block_shift)) * a.Hkv + c) << a.block_shift) + (rho & ((1 << a.block_shift) - 1));
     const auto at = [&](int s) { return at0 + ((int64_t)s * n_blocks * a.Hkv << a.block_shift); };
-    State st{kNegBig, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    State st{kNothingSeen, 0.f, {0.f, 0.f, 0.f, 0.f}};
     constexpr int kStep = kSpread > 1 ? kParts : 1;
     for (int s0 = kSpread > 1 ? part : 0; s0 < n_splits; s0 += kStep * kAtOnce) {
       float m[kAtOnce], l[kAtOnce];
@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combi
       }
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u)
-        if (s0 + kStep * u < n_splits) add(st, m[u], l[u], o[u]);
+        if (s0 + kStep * u < n_splits) add(st, m[u], l[u], o[u], a.scale_log2);
     }
     if constexpr (kSpread > 1) {
       *(f32x4 *)&sum_o[part][at4] = st.o;
@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combi
       st.o = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
       for (int k = 0; k < n; ++k) {
-        const float f = fast_exp2(sum_ml[k][0] - st.top);
+        const float f = factor(sum_ml[k][0], st.top, a.scale_log2);
         st.l = fmaf(sum_ml[k][1], f, st.l);
         st.o += *(const f32x4 *)&sum_o[k][at4] * f;
       }
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combi
       *(f32x4 *)((float *)a.out + to * kD + at4) = x;
     else
       *(u32x2 *)((bf16_t *)a.out + to * kD + at4) = (u32x2){pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
-    if (a.lse && at4 == 0) a.lse[to] = none ? -INFINITY : (st.top + fast_log2(st.l)) * kLn2;
+    if (a.lse && at4 == 0) a.lse[to] = none ? -INFINITY : log_sum(st.top, a.scale_log2, st.l);
   }
 }
 

@@ -25,6 +25,21 @@ __device__ __forceinline__ int wave_scan(int v) {
 }
 __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
+// Weights of a row are 2^((score - m) * scale): about m, the largest score so far or one up to kSlack less, unscaled.  The difference comes first:
+// about a scaled and rounded point the largest weight would be 2 to what the rounding took off, infinite or 0 once half a step
+// of the point passes 128.  A row that has seen nothing stands at the lowest finite score.
+constexpr float kNothingSeen = -3.402823466e38f;
+constexpr float kSlack = 8.0f;            // log2 units
+// What weights about `from` are multiplied by to stand about `to`
+__device__ __forceinline__ float factor(float from, float to, float scale_log2) { return fast_exp2((from - to) * scale_log2); }
+// m * scale, finite
+__device__ __forceinline__ float scaled(float m, float scale_log2) { return fminf(fmaxf(m * scale_log2, kNothingSeen), -kNothingSeen); }
+// Natural logarithm of a sum of weights l about m, the scaled m to twice fp32's bits
+__device__ __forceinline__ float log_sum(float m, float scale_log2, float l) {
+  const float r = scaled(m, scale_log2);
+  return (r + (fmaf(m, scale_log2, -r) + fast_log2(l))) * kLn2;
+}
+
 struct Request {
   int row0, n_all, n, L, past;     // first row; new tokens; those computed; tokens in the cache; position of the first new one
 };

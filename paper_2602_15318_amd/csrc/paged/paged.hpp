@@ -48,7 +48,7 @@ struct ChunkArgs {
   int32_t block_shift;     // log2 of the rows of a block
   int32_t slots, round;    // pieces per KV head that the blocks of rows may be cut into (0: one piece each); those that run at once
   float scale_log2, inv_g;
-  float *part_o, *part_ml; // [piece * Hkv + KV head][row of the block]: unnormalised output [d]; reference point (log2), sum
+  float *part_o, *part_ml; // [piece * Hkv + KV head][row of the block]: unnormalised output [d]; reference score, sum
 };
 // How a call of these sizes is run: rows per block, blocks per KV head at most, pieces, wavefronts per workgroup
 // (blocks of 16 rows), floats of part_o and part_ml.
