@@ -70,7 +70,8 @@ typedef struct {
  *  status      dev int32 out [1]: 0; p > 0: p pages are missing; -1: more new tokens than n_rows; -2: a length out of
  *              range; -3: n_free out of range, or more pages given back than capacity holds.  With a status other than 0
  *              nothing is taken or given back, cu_new is all 0 and every slot -1: what follows in the stream has no rows.
- *  The ids are copied as they are.  Two entries of the batch must not hold the same page.  B = 0: nothing is enqueued.
+ *  The ids are copied as they are.  Two entries of the batch must not hold the same page.
+ *  B = 0: nothing is enqueued, the outputs stay as they were (slots of a step before would be written to again: the binding clears them).
  */
 int sparrow_page_update(const int32_t *old_len, const int32_t *new_len, int32_t B, int32_t page_size,
                         int32_t *block_table, int32_t table_width, int64_t table_stride, int32_t *free_pages,

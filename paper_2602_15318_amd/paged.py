@@ -178,7 +178,7 @@ class _Call:
 def page_update(old_len, new_len, block_table, free_pages, n_free, page_size: int, n_rows: int, pos_offset=None, outputs=None,
                 stream=None):
     """sparrow_page_update: requests from old_len to new_len tokens (int32 [B]); block_table [B, width], free_pages [capacity]
-    and n_free [1] are changed in place.  n_rows: the rows that the new tokens are given, at least as many.
+    and n_free [1] are changed in place.  n_rows: the rows that the new tokens are given, at least as many.  No requests: rows of nobody.
     Returns int32 tensors (slots [n_rows], cu_new [B+1], positions [n_rows], status [1]), or fills `outputs`, four such."""
     r = _native.page_update(old_len, new_len, block_table, free_pages, n_free, page_size, n_rows, pos_offset, outputs, stream)
     if r is not NotImplemented:
@@ -196,8 +196,7 @@ def page_update(old_len, new_len, block_table, free_pages, n_free, page_size: in
     width, stride = _table(block_table, B)
     made = ()
     if outputs is None:
-        new = torch.zeros if B == 0 else torch.empty
-        made = outputs = tuple(new(n, dtype=torch.int32, device=dev) for n in (n_rows, B + 1, n_rows, 1))
+        made = outputs = tuple(torch.empty(n, dtype=torch.int32, device=dev) for n in (n_rows, B + 1, n_rows, 1))
     slots, cu_new, positions, status = outputs
     for name, t, n in (("slots", slots, n_rows), ("cu_new", cu_new, B + 1), ("positions", positions, n_rows), ("status", status, 1)):
         _ints(name, t, n)
@@ -205,6 +204,10 @@ def page_update(old_len, new_len, block_table, free_pages, n_free, page_size: in
         _check(lib.sparrow_page_update(_ptr(old_len), _ptr(new_len), B, int(page_size), _ptr(block_table), width, stride,
                                        _ptr(free_pages), free_pages.shape[0], _ptr(n_free), _ptr(pos_offset), int(n_rows),
                                        _ptr(slots), _ptr(positions), _ptr(cu_new), _ptr(status), handle))
+        if B == 0:                          # nothing was enqueued, and every row is nobody's
+            with torch.cuda.stream(stream):
+                for t, x in ((slots, -1), (positions, 0), (cu_new, 0), (status, 0)):
+                    t.fill_(x)
     return slots, cu_new, positions, status
 
 
