@@ -2,7 +2,8 @@
 
 Function names and argument order follow include/sparrow_paged.h.  Tensors are torch tensors on one GPU; only the rotary
 frequencies and their axes are host arrays.  There is no fallback: if the HIP library has not been built, importing this module
-raises.  A call runs on the current stream of its tensors' device, or on `stream`.
+raises.  A call runs on the current stream of its tensors' device, or on `stream`, a stream of that device; as with any two
+streams, the caller orders it behind what makes the arguments and before what reads the results.
 
 Calls whose arguments are plain go through _native_paged.so (csrc/paged/binding_paged.cpp): it does the checks and the marshalling below
 in C++ and returns NotImplemented for everything else.
@@ -152,25 +153,36 @@ def _axes(positions, N, inv_freq, freq_axis, d):
 
 
 class _Call:
-    """The device and stream of a call: `with _Call(device, stream, tensors allocated here) as handle`."""
+    """The device and stream of a call: `with _Call(device, stream) as call`.  What is allocated inside belongs to the call's stream, so that
+    nothing queued on another one still uses the memory; what the caller gets of it goes through call.given()."""
 
-    def __init__(self, device, stream, *made):
-        self.device, self.stream, self.made = device, stream, made
+    def __init__(self, device, stream):
+        if stream is not None and stream.device != device:
+            raise ValueError("the stream must be one of the tensors' GPU")
+        self.device, self.stream, self.on = device, stream, None
 
     def __enter__(self):
         current = torch.cuda.current_device()
         self.back = None if self.device.index == current else current
-        raw = torch._C._cuda_getCurrentRawStream(self.device.index)
-        if self.stream is not None and self.stream.cuda_stream != raw:
-            raw = self.stream.cuda_stream
-            for t in self.made:             # freed, it may be handed out again only once that stream has passed
-                if t is not None:
-                    t.record_stream(self.stream)
         if self.back is not None:
             torch.cuda.set_device(self.device)
-        return raw
+        self.handle = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if self.stream is not None and self.stream.cuda_stream != self.handle:
+            self.handle = self.stream.cuda_stream
+            self.caller = torch.cuda.current_stream(self.device)
+            self.on = torch.cuda.stream(self.stream)
+            self.on.__enter__()
+        return self
 
-    def __exit__(self, *_):
+    def given(self, t):
+        """A tensor allocated here that the caller goes on using: freed, it is handed out again only once the caller's stream has passed."""
+        if self.on is not None:
+            t.record_stream(self.caller)
+        return t
+
+    def __exit__(self, *error):
+        if self.on is not None:
+            self.on.__exit__(*error)
         if self.back is not None:
             torch.cuda.set_device(self.back)
 
@@ -194,20 +206,18 @@ def page_update(old_len, new_len, block_table, free_pages, n_free, page_size: in
     if pos_offset is not None:
         _ints("pos_offset", pos_offset, B)
     width, stride = _table(block_table, B)
-    made = ()
-    if outputs is None:
-        made = outputs = tuple(torch.empty(n, dtype=torch.int32, device=dev) for n in (n_rows, B + 1, n_rows, 1))
-    slots, cu_new, positions, status = outputs
-    for name, t, n in (("slots", slots, n_rows), ("cu_new", cu_new, B + 1), ("positions", positions, n_rows), ("status", status, 1)):
-        _ints(name, t, n)
-    with _Call(dev, stream, *made) as handle:
+    with _Call(dev, stream) as call:
+        if outputs is None:
+            outputs = tuple(call.given(torch.empty(n, dtype=torch.int32, device=dev)) for n in (n_rows, B + 1, n_rows, 1))
+        slots, cu_new, positions, status = outputs
+        for name, t, n in (("slots", slots, n_rows), ("cu_new", cu_new, B + 1), ("positions", positions, n_rows), ("status", status, 1)):
+            _ints(name, t, n)
         _check(lib.sparrow_page_update(_ptr(old_len), _ptr(new_len), B, int(page_size), _ptr(block_table), width, stride,
                                        _ptr(free_pages), free_pages.shape[0], _ptr(n_free), _ptr(pos_offset), int(n_rows),
-                                       _ptr(slots), _ptr(positions), _ptr(cu_new), _ptr(status), handle))
+                                       _ptr(slots), _ptr(positions), _ptr(cu_new), _ptr(status), call.handle))
         if B == 0:                          # nothing was enqueued, and every row is nobody's
-            with torch.cuda.stream(stream):
-                for t, x in ((slots, -1), (positions, 0), (cu_new, 0), (status, 0)):
-                    t.fill_(x)
+            for t, x in ((slots, -1), (positions, 0), (cu_new, 0), (status, 0)):
+                t.fill_(x)
     return slots, cu_new, positions, status
 
 
@@ -220,17 +230,16 @@ def mrope_table(positions, inv_freq, freq_axis, cos=None, sin=None, stream=None)
     N = positions.shape[-1]
     n_axes, stride, inv_freq, freq_axis, d = _axes(positions, N, inv_freq, freq_axis, None)
     dev = _tensors(positions, cos, sin)
-    made = []
-    if cos is None:
-        made.append(cos := torch.empty((N, d // 2), dtype=torch.float32, device=dev))
-    if sin is None:
-        made.append(sin := torch.empty((N, d // 2), dtype=torch.float32, device=dev))
     for t in (cos, sin):
-        if t.dtype != torch.float32 or tuple(t.shape) != (N, d // 2) or not t.is_contiguous():
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (N, d // 2) or not t.is_contiguous()):
             raise ValueError("cos and sin must be contiguous float32 [N, d/2]")
-    with _Call(dev, stream, *made) as handle:
+    with _Call(dev, stream) as call:
+        if cos is None:
+            cos = call.given(torch.empty((N, d // 2), dtype=torch.float32, device=dev))
+        if sin is None:
+            sin = call.given(torch.empty((N, d // 2), dtype=torch.float32, device=dev))
         _check(lib.sparrow_mrope_table(_ptr(positions), stride, n_axes, inv_freq.ctypes.data, freq_axis.ctypes.data, d, N,
-                                       _ptr(cos), _ptr(sin), handle))
+                                       _ptr(cos), _ptr(sin), call.handle))
     return cos, sin
 
 
@@ -250,16 +259,15 @@ def mrope_append(q, k, v, positions, inv_freq, freq_axis, slots, k_cache, v_cach
     _ints("slots", slots, N)
     n_axes, stride, inv_freq, freq_axis, _ = _axes(positions, N, inv_freq, freq_axis, d)
     dev = _tensors(q, k, v, positions, slots, k_cache, v_cache, q_out)
-    made = None
-    if q_out is None:
-        made = q_out = torch.empty((N, hq, d), dtype=q.dtype, device=dev)
-    elif q_out.dtype != q.dtype or q_out.shape != q.shape or not q_out.is_contiguous():
+    if q_out is not None and (q_out.dtype != q.dtype or q_out.shape != q.shape or not q_out.is_contiguous()):
         raise ValueError("q_out must be contiguous [N, Hq, d] of q's dtype")
     desc = PagedDesc(_CODES[q.dtype], hq, hkv, d, 0.0, page, n_pages, s_page, s_tok, s_head, q_row, kv_row)
-    with _Call(dev, stream, made) as handle:
+    with _Call(dev, stream) as call:
+        if q_out is None:
+            q_out = call.given(torch.empty((N, hq, d), dtype=q.dtype, device=dev))
         _check(lib.sparrow_mrope_append(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(positions), stride, n_axes,
                                         inv_freq.ctypes.data, freq_axis.ctypes.data, _ptr(slots), N, _ptr(q_out), _ptr(k_cache),
-                                        _ptr(v_cache), handle))
+                                        _ptr(v_cache), call.handle))
     return q_out
 
 
@@ -284,25 +292,24 @@ def chunk_attn(q, k_cache, v_cache, block_table, cu_new, kv_len, max_new: int, s
     _ints("cu_new", cu_new, B + 1)
     width, table_stride = _table(block_table, B)
     dev = _tensors(q, k_cache, v_cache, block_table, cu_new, kv_len, out, lse, workspace)
-    made = []
-    if out is None:
-        made.append(out := torch.empty((rows, hq, d), dtype=q.dtype, device=dev))
-    elif out.dtype != q.dtype or out.shape != q.shape or not out.is_contiguous():
+    if out is not None and (out.dtype != q.dtype or out.shape != q.shape or not out.is_contiguous()):
         raise ValueError("out must be contiguous [rows, Hq, d] of q's dtype")
-    if lse is None and want_lse:
-        made.append(lse := torch.empty((rows, hq), dtype=torch.float32, device=dev))
-    elif lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (rows, hq) or not lse.is_contiguous()):
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (rows, hq) or not lse.is_contiguous()):
         raise ValueError("lse must be contiguous float32 [rows, Hq]")
     desc = PagedDesc(_CODES[q.dtype], hq, hkv, d, float(scale), page, n_pages, s_page, s_tok, s_head, q_row, 0)
-    if workspace is None:
-        need = lib.sparrow_chunk_attn_workspace(ctypes.byref(desc), B, rows, int(max_new))
-        if need:
-            made.append(workspace := torch.empty(need, dtype=torch.uint8, device=dev))
-    elif not workspace.is_contiguous():
+    if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    with _Call(dev, stream, *made) as handle:
+    with _Call(dev, stream) as call:
+        if out is None:
+            out = call.given(torch.empty((rows, hq, d), dtype=q.dtype, device=dev))
+        if lse is None and want_lse:
+            lse = call.given(torch.empty((rows, hq), dtype=torch.float32, device=dev))
+        if workspace is None:
+            need = lib.sparrow_chunk_attn_workspace(ctypes.byref(desc), B, rows, int(max_new))
+            if need:
+                workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         _check(lib.sparrow_chunk_attn(ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), width,
                                       table_stride, _ptr(cu_new), _ptr(kv_len), B, rows, int(max_new), _ptr(out), _ptr(lse),
                                       _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                      handle))
+                                      call.handle))
     return out, lse
