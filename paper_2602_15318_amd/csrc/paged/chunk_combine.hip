@@ -26,27 +26,32 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) chunk_combi
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.y + 32768 * blockIdx.z;
   if (r >= a.n_rows) return;
-  const Plan p = make_plan(a, lane);
-  int b = -1, n_blocks = 0, n_splits = 0, first = 0;
-  Request q{};
+  // the row's request, and what the first pass has left of it
+  int b = -1, i = 0, n = 0, past = 0, first = 0, n_splits = 0;
 #pragma unroll
   for (int k = 0; k < kMaxPerLane; ++k)
     if (b < 0 && 64 * k < a.B) {
-      const unsigned long long m = __builtin_amdgcn_ballot_w64(r >= p.rq[k].row0 && r - p.rq[k].row0 < p.rq[k].n);
+      Request q{};
+      int2 plan{};
+      if (64 * k + lane < a.B) {
+        q = request_of(a, 64 * k + lane);
+        plan = ((const int2 *)a.plan)[64 * k + lane];
+      }
+      const unsigned long long m = __builtin_amdgcn_ballot_w64(r >= q.row0 && r - q.row0 < q.n);
       if (m != 0ull) {
         const int l = __builtin_ctzll(m);
         b = 64 * k + l;
-        n_blocks = lane_value(p.n_blocks[k], l);
-        n_splits = lane_value(p.n_splits[k], l);
-        first = lane_value(p.end[k], l) - n_blocks * n_splits;
-        q = {lane_value(p.rq[k].row0, l), lane_value(p.rq[k].n_all, l), lane_value(p.rq[k].n, l), lane_value(p.rq[k].L, l),
-             lane_value(p.rq[k].past, l)};
+        i = r - lane_value(q.row0, l);
+        n = lane_value(q.n, l);
+        past = lane_value(q.past, l);
+        first = lane_value(plan.x, l);
+        n_splits = lane_value(plan.y, l);
       }
     }
-  if (b < 0 || n_splits == 1) return;                      // (in one piece: written already)
-  if (first < 0 || first + n_blocks * n_splits > a.slots) return;      // (offsets that overlap promise any number of pieces)
-  const int i = r - q.row0;
-  const bool none = q.past + i < 0;
+  if (b < 0 || n_splits <= 1) return;                      // (in one piece: written already)
+  const int n_blocks = blocks_of(a, n);
+  if (first < 0 || (int64_t)n_blocks * n_splits > a.slots - first) return;     // (offsets that overlap: a plan that nobody has written)
+  const bool none = past + i < 0;
   const int part = w * kGroups + group;                    // kSpread 1: the head; else which of the pieces
   for (int h = kSpread > 1 ? (int)blockIdx.x : part; h < a.Hq; h += kSpread > 1 ? a.Hq : 4 * kGroups) {
     const int c = quotient(h, a.g, a.inv_g), rho = i * a.g + h - c * a.g;

@@ -1,5 +1,7 @@
-// Which piece of the batch a workgroup of the chunk attention takes.  Lengths live on the device, so the workgroups work the
-// plan out themselves, each the same one: a wavefront holds a request per lane (and register, above 64 requests).
+// Which piece of the batch a workgroup of the chunk attention takes.  Lengths live on the device, so the workgroups of the first pass work the
+// plan out themselves, each the same one: a wavefront holds a request per lane (and register, above 64 requests).  The second pass, another
+// kernel, must not depend on its floating-point operations coming out the same there: the workgroup of a request's first piece leaves
+// the request's part of the plan in the workspace.
 //
 // A row is a (new token, query head of the group) pair; the rows of a request and KV head are cut into blocks, a
 // block's keys into pieces of T tokens at most, T as small as it may be for the sum over the blocks of ceil(length / T) to be at
@@ -64,6 +66,11 @@ __device__ __forceinline__ int quotient(int x, int y) {
   return __builtin_amdgcn_readfirstlane(quotient(x, y, __builtin_amdgcn_rcpf((float)y)));
 }
 
+// Blocks of the rows of n new tokens
+__device__ __forceinline__ int blocks_of(const ChunkArgs &a, int n) {
+  return (int)(((int64_t)n * a.g + (1 << a.block_shift) - 1) >> a.block_shift);
+}
+
 struct Piece {
   Request rq;
   int b, block, n_blocks, split, n_splits, first, t0, t1;    // first: number of the request's first piece
@@ -94,7 +101,7 @@ __device__ __forceinline__ Plan make_plan(const ChunkArgs &a, int lane) {
     if (64 * k < a.B) {
       if (64 * k + lane < a.B) {
         p.rq[k] = request_of(a, 64 * k + lane);
-        p.n_blocks[k] = (int)(((int64_t)p.rq[k].n * a.g + (1 << a.block_shift) - 1) >> a.block_shift);
+        p.n_blocks[k] = blocks_of(a, p.rq[k].n);
       }
       blocks += min(p.n_blocks[k], a.slots);               // (offsets that overlap may promise any number)
       weight += (float)p.n_blocks[k] * (float)p.rq[k].L;
@@ -171,6 +178,10 @@ __device__ __forceinline__ bool find_piece(const ChunkArgs &a, int idx, int lane
   const int each = (quotient(q.rq.L + q.n_splits - 1, q.n_splits) + kGrain - 1) / kGrain * kGrain;
   q.t0 = min(q.rq.L, q.split * each);
   q.t1 = min(q.rq.L, q.t0 + each);
+  if (a.plan && idx == q.first && blockIdx.x == 0 && threadIdx.x == 0) {
+    a.plan[2 * q.b] = q.first;
+    a.plan[2 * q.b + 1] = q.n_splits;
+  }
   *out = q;
   return true;
 }

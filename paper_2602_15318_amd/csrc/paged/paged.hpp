@@ -49,6 +49,7 @@ struct ChunkArgs {
   int32_t slots, round;    // pieces per KV head that the blocks of rows may be cut into (0: one piece each); those that run at once
   float scale_log2, inv_g;
   float *part_o, *part_ml; // [piece * Hkv + KV head][row of the block]: unnormalised output [d]; reference score, sum
+  int32_t *plan;           // [B][2]: a request's first piece, pieces of each of its blocks; NULL where nothing is cut
 };
 // How a call of these sizes is run: rows per block, blocks per KV head at most, pieces, wavefronts per workgroup
 // (blocks of 16 rows), floats of part_o and part_ml.

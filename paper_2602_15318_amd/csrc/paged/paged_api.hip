@@ -185,7 +185,7 @@ size_t sparrow_chunk_attn_workspace(const sparrow_paged_desc *desc, int32_t B, i
       max_new <= 0)
     return 0;
   const ChunkShape s = chunk_shape(desc->dtype, desc->head_dim, desc->n_q_heads, desc->n_kv_heads, B, n_rows, max_new, SPARROW_MAX_PAGED_TOKENS);
-  return round_up((size_t)s.floats_o * 4, 256) + round_up((size_t)s.floats_ml * 4, 256);
+  return s.slots == 0 ? 0 : round_up((size_t)s.floats_o * 4, 256) + round_up((size_t)s.floats_ml * 4, 256) + round_up((size_t)B * 8, 256);
 }
 
 int sparrow_chunk_attn(const sparrow_paged_desc *desc, const void *q, const void *k_cache, const void *v_cache,
@@ -226,6 +226,7 @@ int sparrow_chunk_attn(const sparrow_paged_desc *desc, const void *q, const void
   a.slots = shape.slots; a.round = shape.round; a.block_shift = shift_of(shape.rows);
   a.part_o = (float *)workspace;
   a.part_ml = (float *)((unsigned char *)workspace + round_up((size_t)shape.floats_o * 4, 256));
+  a.plan = shape.slots == 0 ? nullptr : (int32_t *)((unsigned char *)a.part_ml + round_up((size_t)shape.floats_ml * 4, 256));
   const hipError_t e = launch_chunk_attn(desc->dtype, desc->head_dim, a, (hipStream_t)hip_stream);
   if (e != hipSuccess) return fail(SPARROW_ERR_DEVICE, "chunk_attn launch: %s", hipGetErrorString(e));
   return SPARROW_OK;
