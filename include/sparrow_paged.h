@@ -123,7 +123,7 @@ int sparrow_mrope_append(const sparrow_paged_desc *desc, const void *q, const vo
  *  Limits: B <= SPARROW_MAX_PAGED_BATCH, table_width * page_size and n_rows <= SPARROW_MAX_PAGED_TOKENS, n_rows * Hq < 2^31.
  *  Values and keys that a row does not see do not reach it, infinities and NaN included.
  *  Scores may be as large as fp32 holds them, unscaled and scaled: among scores whose distances pass what fp32 resolves, the largest takes all.
- *  B = 0, n_rows = 0 or max_new = 0: nothing is enqueued.
+ *  B = 0, n_rows = 0 or max_new = 0: nothing is enqueued.  The workspace of sizes that the call refuses is 0 bytes.
  */
 size_t sparrow_chunk_attn_workspace(const sparrow_paged_desc *desc, int32_t B, int32_t n_rows, int32_t max_new);
 int sparrow_chunk_attn(const sparrow_paged_desc *desc, const void *q, const void *k_cache, const void *v_cache,

@@ -181,7 +181,10 @@ int sparrow_mrope_append(const sparrow_paged_desc *desc, const void *q, const vo
 }
 
 size_t sparrow_chunk_attn_workspace(const sparrow_paged_desc *desc, int32_t B, int32_t n_rows, int32_t max_new) {
-  if (!desc || desc->n_q_heads <= 0 || desc->n_kv_heads <= 0 || desc->n_q_heads % desc->n_kv_heads != 0 || B <= 0 || n_rows <= 0 ||
+  // (sizes that the call refuses would overflow what is worked out from them)
+  if (!desc || (desc->dtype != SPARROW_F32 && desc->dtype != SPARROW_BF16) || (desc->head_dim != 64 && desc->head_dim != 128) ||
+      desc->n_q_heads <= 0 || desc->n_q_heads > 1 << 15 || desc->n_kv_heads <= 0 || desc->n_q_heads % desc->n_kv_heads != 0 || B <= 0 ||
+      B > SPARROW_MAX_PAGED_BATCH || n_rows <= 0 || n_rows > SPARROW_MAX_PAGED_TOKENS || (int64_t)n_rows * desc->n_q_heads >= 1ll << 31 ||
       max_new <= 0)
     return 0;
   const ChunkShape s = chunk_shape(desc->dtype, desc->head_dim, desc->n_q_heads, desc->n_kv_heads, B, n_rows, max_new, SPARROW_MAX_PAGED_TOKENS);
