@@ -121,6 +121,8 @@ int sparrow_mrope_append(const sparrow_paged_desc *desc, const void *q, const vo
  *  workspace    dev, 256-byte aligned, at least sparrow_chunk_attn_workspace() bytes; calls that may run at the same time
  *               need one each
  *  Limits: B <= SPARROW_MAX_PAGED_BATCH, table_width * page_size and n_rows <= SPARROW_MAX_PAGED_TOKENS, n_rows * Hq < 2^31.
+ *  Scores, weights' sums and partial results are fp32; in bf16 a weight is rounded once, for its product with V (row sums take it unrounded), and
+ *  the output once.
  *  Values and keys that a row does not see do not reach it, infinities and NaN included.
  *  Scores may be as large as fp32 holds them, unscaled and scaled: among scores whose distances pass what fp32 resolves, the largest takes all.
  *  B = 0, n_rows = 0 or max_new = 0: nothing is enqueued.  The workspace of sizes that the call refuses is 0 bytes.

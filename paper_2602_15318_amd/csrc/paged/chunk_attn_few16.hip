@@ -1,6 +1,6 @@
 // Attention of few new tokens over the paged cache by 16-row tiles: up to 16 rows (new token, query head of the group) per request and KV head, in
 // fp32 up to 32.  Bound by memory: 28/4 heads of 128, 48 single tokens over up to 8,192 (405 MB) 69 us, 5.9 TB/s; one over 26,112 (53.5 MB) 11, 4.9
-// TB/s with launch, plan and first tile in it; the second pass takes 5 to 6.5 more.  16-row tiles against 32-row ones for up to 16 rows: 79 / 83 and
+// TB/s with launch, plan and first tile in it; the second pass takes 4.5 to 5 more.  16-row tiles against 32-row ones for up to 16 rows: 79 / 83 and
 // 17.3 / 18.1 us a call; for 28 rows over 26,112 tokens 27 / 18, so that more rows take 32-row tiles (chunk_attn_few32.hip).
 //
 // A workgroup takes one block and piece of keys; its wavefronts take the 16-token tiles in turn and know nothing of each other until the
@@ -165,7 +165,9 @@ __global__ void __launch_bounds__(64 * kWaves) chunk_few16_kernel(ChunkArgs a) {
           }
         }
       } else {
-        // probabilities are rounded to bf16 for the product (their sum is not): 2^-9 of a term on average, of the result less
+        // Probabilities are rounded to bf16 for the product (their sum is not): 2^-9 of a term on average, of the result less.  A second bf16 term of
+        // each, with the test for values that are no numbers that it needs in every tile: 48 single tokens 73.0 -> 74.5 us, 200 90 -> 95, forty over
+        // 500 13.1 -> 15.9, twelve chains in 32-row tiles 33.5 -> 55.7.
         const int row = 4 * c4 + (n16 >> 2);
         bf16x4 v[kDB];
 #pragma unroll

@@ -1,6 +1,7 @@
 // Attention of few new tokens over the paged cache, bf16: 17 to 64 rows (new token, query head of the group) per request and KV head.
 // Bound by memory: every key and value is read once, by one workgroup.  Measured a call, 28/4 heads of 128: four tokens over 26,112 (53.5 MB) 18 us,
-// eight 23, twelve requests of eight tokens over up to 8,000 34.  Probabilities are rounded to bf16 for the output's product; their sum is not.
+// eight 23, twelve requests of eight tokens over up to 8,000 34.  Probabilities are rounded to bf16 for the output's product; their sum is not (what a
+// second term costs: chunk_attn_few16.hip).
 //
 // A workgroup of four wavefronts takes one piece of a request's keys for one KV head; the wavefronts take its 32-token tiles in turn
 // and know nothing of each other until the end, where their four states of a row are merged through LDS.  A wavefront's tiles travel

@@ -9,7 +9,7 @@
 //
 // Probabilities are rounded to bf16 for the output's product, half a step 2^-9 to 2^-8 of a term; the row's sum takes them unrounded.
 //
-// Measured: that chunk 625 to 690 us by card (1,070 to 1,180 TFLOP/s; matrix cores busy 57 % of the cycles), prompt of 7,001 tokens 325 to 365
+// Measured: that chunk 625 to 690 us by card (1,070 to 1,180 TFLOP/s; matrix cores busy 56 % of the cycles), prompt of 7,001 tokens 325 to 365
 // (960 to 1,080; 53 %), prompt of 6,000 with 32/8 heads of 64 190 to 204.
 #include "chunk_attn_mfma.hpp"
 

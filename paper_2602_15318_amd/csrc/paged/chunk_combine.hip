@@ -1,8 +1,8 @@
 // Second pass of the chunk attention: the pieces of a block's keys put together.  kD / 4 lanes take a row's piece, 16 bytes each; the groups of
 // kSpread wavefronts (8 or 2) share the pieces of one (row of the batch, query head), the loads of up to 8 pieces of a group on their
 // way at once.  Where there are many rows (kSpread 1), each group takes a head of its own.
-// Measured, 28/4 heads of 128: one token over 26,112 5 us, 48 over up to 8,192 6.5: about a launch and two dependent round trips.  A mixed batch of
-// nine, 32/8 heads of 64, 10.
+// Measured, 28/4 heads of 128: one token over 26,112 4.5 us, 48 over up to 8,192 5.0: about a launch and two dependent round trips.  A mixed batch of
+// nine, 32/8 heads of 64, 7.2.
 #include "chunk_plan.hpp"
 
 namespace sparrow {

@@ -114,7 +114,9 @@ __device__ __forceinline__ Plan make_plan(const ChunkArgs &a, int lane) {
   for (int round = 1; round * a.round <= a.slots; ++round) {
     const int N = round * a.round;
     if (N <= U) continue;
-    // T1 = W / (N - U) always fits; the smallest that does lies between W / N and it, and is looked for where they differ by much.
+    // T1 = W / (N - U) always fits; the smallest that does lies between W / N and it, and is looked for where they differ by much (N
+    // below 8 U.  Never: chunk of 512 beside 16 single tokens 107 -> 126 us, of 300 beside 4 51 -> 59, twelve chains 33.6 -> 32.9; always: eight single
+    // tokens 19.6 -> 19.9, chunk of 256 over 8,192 53.3 -> 52.4).
     // (the factor: the sum is off by 2^-16 at most)
     const auto grains = [&](float t) { return (min((int)(t * (1.f + 0x1p-14f)), 1 << 28) + kGrain) / kGrain; };
     int hi = grains(W / (float)(N - U));
@@ -130,7 +132,8 @@ __device__ __forceinline__ Plan make_plan(const ChunkArgs &a, int lane) {
         else lo = mid;
       }
     }
-    const int cost = round * (hi + (a.block_shift == 8 ? 2 : 4));    // (so many grains a piece's beginning and end take)
+    const int cost = round * (hi + (a.block_shift == 8 ? 2 : 4));    // (so many grains a piece's beginning and end take: 0 to 4
+                                                                     // make no difference, 8 one round of an fp32 chunk, 214 -> 259 us)
     if (cost < best) {
       best = cost;
       p.T = hi * kGrain;

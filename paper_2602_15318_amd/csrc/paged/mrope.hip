@@ -40,9 +40,9 @@ __global__ void __launch_bounds__(256) mrope_table_kernel(RopeTableArgs a, Frequ
   a.sin[at] = t.s;
 }
 
-// A workgroup takes one token: its angles once, then q's and k's heads by 16 bytes of each half, v's by two times 16 bytes.
 // A workgroup takes a token: its angles once, then 16 bytes of both halves of a head per thread.  Bound by memory: 8,192 tokens of 28/4 heads of
-// 128, bf16, 151 MB read and written, 31.6 us a call among others (4.8 TB/s, a large copy 5.05), 24.3 with the inputs in the Infinity Cache.
+// 128, bf16, 151 MB read and written, 31.6 us a call among others (4.8 TB/s, a large copy 5.05), 24.3 with the inputs in the Infinity Cache; in fp32 82
+// behind other work on memory (bf16 44 there).
 template <typename T, int kD>
 __global__ void __launch_bounds__(256) mrope_append_kernel(AppendArgs a, Frequencies f) {
   constexpr int kHalf = kD / 2, kPer = Elem<T>::kPer16B, kParts = kHalf / kPer;

@@ -110,3 +110,8 @@ def test_pages_and_slots_of_large_pages(sp, page):
     at = got[0][:rows - 3].long()
     assert torch.equal(kc.view(-1, Hkv, d)[at], k[:rows - 3]) and torch.equal(vc.view(-1, Hkv, d)[at], k[:rows - 3])
     assert int((kc != 0).any(-1).any(-1).sum()) == rows - 3
+
+
+@pytest.mark.parametrize("dtype, new, page", [("bf16", 1, 16), ("bf16", 20, 4096), ("bf16", 70, 64), ("f32", 1, 4096), ("f32", 40, 16)])
+def test_the_longest_request_there_is(sp, dtype, new, page):
+    _check(sp, ref.Batch([1 << 22, 40 + new], [new, new], dtype, 2, 1, 64, page, seed=new))
