@@ -164,3 +164,33 @@ def test_results_stay_until_the_caller_s_stream_has_passed():
     assert not at & {t.data_ptr() for t in second}
     torch.cuda.synchronize()
     assert [float(s) for s in sums] == [3000 * 32.0, 0.0]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", NAMES)
+def test_captured_on_a_stream_of_its_own(name):
+    """A call on a side stream that a capture has drawn in: replays give what an eager call gives, with eager work in between."""
+    args = _args(name, "cuda")
+    if name == "chunk_attn":
+        for t in args[:3]:
+            t.normal_()
+    state = [t.clone() if isinstance(t, torch.Tensor) else t for t in args]
+    want = getattr(paged, name)(*state)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        got = getattr(paged, name)(*args, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+    first = [t.clone() if isinstance(t, torch.Tensor) else t for t in args]
+    for _ in range(3):
+        for t, x in zip(args, first):
+            if isinstance(t, torch.Tensor):
+                t.copy_(x)
+        for t in got if isinstance(got, tuple) else (got,):
+            t.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        for g, w in zip(got if isinstance(got, tuple) else (got,), want if isinstance(want, tuple) else (want,)):
+            assert torch.equal(g, w)
+        torch.zeros(1 << 20, device="cuda").add_(1)
