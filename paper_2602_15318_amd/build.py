@@ -1,5 +1,5 @@
 """Build the HIP libraries (gfx950) and the binding's native parts in-tree: paper_2602_15318_amd/libsparrow.so,
-libsparrow_paged.so, _native.so, _native_paged.so."""
+libsparrow_paged.so, libsparrow_serve.so, _native.so, _native_paged.so, _native_serve.so."""
 from __future__ import annotations
 
 import concurrent.futures
@@ -14,8 +14,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparrow.so")
 PAGED = os.path.join(HERE, "libsparrow_paged.so")
+SERVE = os.path.join(HERE, "libsparrow_serve.so")
 NATIVE = os.path.join(HERE, "_native.so")
 NATIVE_PAGED = os.path.join(HERE, "_native_paged.so")
+NATIVE_SERVE = os.path.join(HERE, "_native_serve.so")
 
 # The preload count puts the leading scalar arguments of a kernel into scalar registers at launch: a
 # wavefront's first load waits for no load of arguments (0.3 to 0.4 us on kernels of 6 to 13 us).
@@ -40,8 +42,8 @@ def _run(cmd, verbose: bool) -> None:
 
 
 def build(verbose: bool = False, extra=()) -> str:
-    """Compile every csrc/*.hip into one shared library, csrc/paged/*.hip into another, and the binding's native
-    part of each.  Always recompiles."""
+    """Compile every csrc/*.hip into one shared library, csrc/paged/*.hip and csrc/serve/*.hip into others, and the binding's
+    native part of each.  Always recompiles."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
     def hip(lib, *under):
@@ -55,9 +57,9 @@ def build(verbose: bool = False, extra=()) -> str:
               "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, *source), "-o", lib,
               "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
 
-    with concurrent.futures.ThreadPoolExecutor(4) as pool:     # side by side: each is one compiler, file after file
-        for done in [pool.submit(hip, LIB), pool.submit(hip, PAGED, "paged"), pool.submit(native, NATIVE, "binding.cpp"),
-                     pool.submit(native, NATIVE_PAGED, "paged", "binding_paged.cpp")]:
+    with concurrent.futures.ThreadPoolExecutor(6) as pool:     # side by side: each is one compiler, file after file
+        for done in [pool.submit(hip, LIB), pool.submit(hip, PAGED, "paged"), pool.submit(hip, SERVE, "serve"), pool.submit(native, NATIVE, "binding.cpp"),
+                     pool.submit(native, NATIVE_PAGED, "paged", "binding_paged.cpp"), pool.submit(native, NATIVE_SERVE, "serve", "binding_serve.cpp")]:
             done.result()
     return LIB
 

@@ -1,0 +1,49 @@
+// Internal interface of the kernels behind include/sparrow_serve.h.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../../include/sparrow_serve.h"
+#include "../paged/paged.hpp"
+
+namespace sparrow {
+
+typedef unsigned char e4m3_t;   // raw bits
+
+struct Append8Args {
+  const void *q, *k, *v;
+  const int32_t *positions, *slots;
+  void *q_out;
+  e4m3_t *k_cache, *v_cache;
+  uint8_t *exponents;
+  int64_t axis_stride, q_row, kv_row, stride_page, stride_token, stride_head;   // elements
+  int32_t N, Hq, Hkv, page_shift, n_slots;
+};
+hipError_t launch_mrope_append8(int dtype, const Append8Args &a, const Frequencies &f, int d, hipStream_t st);
+
+struct GatherArgs {
+  const void *k, *v;
+  const uint8_t *exponents;                               // NULL: caches of the outputs' type
+  const int32_t *block_table, *first, *cu_rows;
+  void *k_out, *v_out;
+  int64_t table_stride, stride_page, stride_token, stride_head, out_row, out_head;    // elements
+  int32_t B, n_rows, Hkv, table_width, page_shift, n_pages;
+};
+hipError_t launch_page_gather(int dtype, int d, const GatherArgs &a, hipStream_t st);
+
+struct ServeArgs {
+  const void *q, *k, *v;
+  const uint8_t *exponents;
+  const int32_t *block_table, *cu_new, *kv_len, *group_start, *prefix_len;
+  void *out;
+  float *lse;
+  int64_t table_stride, q_row, stride_page, stride_token, stride_head;          // elements
+  int32_t B, G, n_rows, max_new, Hq, Hkv, g, table_width, page_shift, n_pages;
+  float scale_log2;
+};
+hipError_t launch_serve_attn(int dtype, int d, const ServeArgs &a, hipStream_t st);
+
+// 2^(byte - 127) of a row of an 8-bit cache, normal and finite whatever the byte
+__device__ __forceinline__ float power_of(unsigned int byte) { return __uint_as_float(min(max(byte, 1u), 254u) << 23); }
+
+}  // namespace sparrow
