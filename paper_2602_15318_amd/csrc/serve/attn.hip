@@ -1,73 +1,49 @@
-// Attention of new tokens over a paged cache of 8 bits or of the model's type: a wavefront per (row of the batch, query head), key by key.
-#include <type_traits>
+// Which kernel runs a call of the attention, and its launches.
+#include <algorithm>
 
-#include "../paged/chunk_plan.hpp"
 #include "serve.hpp"
 
 namespace sparrow {
 
-namespace {
+hipError_t launch_serve_bf16(int d, int blocks, const ServeArgs &a, hipStream_t st);
+hipError_t launch_serve_f32(int d, int blocks, const ServeArgs &a, hipStream_t st);
+hipError_t launch_serve_combine(int dtype, int d, const ServeArgs &a, hipStream_t st);
 
-template <typename T, typename C, int kD>
-__global__ void __launch_bounds__(64) serve_attn_plain_kernel(ServeArgs a) {
-  constexpr int kPer = kD / 64;
-  const int lane = threadIdx.x, h = blockIdx.x, r = blockIdx.y + 32768 * blockIdx.z, c = h / a.g;
-  if (r >= a.n_rows) return;
-  int b = -1, i = 0, past = 0;
-  for (int k = 0; k < a.B && b < 0; ++k) {
-    const int c0 = min(max(a.cu_new[k], 0), a.n_rows), c1 = min(max(a.cu_new[k + 1], 0), a.n_rows);
-    if (r >= c0 && r < c1) {
-      b = k;
-      i = r - c0;
-      past = max(a.kv_len[k], 0) - (c1 - c0);
-    }
+ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t n_rows, int max_new, int64_t capacity) {
+  ServeShape s;
+  const bool f32 = dtype == SPARROW_F32;
+  const int g = Hq / Hkv;
+  const int64_t most = std::min<int64_t>(max_new, n_rows) * g;                 // rows of a request, at most
+  const int64_t of_item = G > 0 ? n_rows * g : most;                           // of an item
+  s.rows = of_item <= 16 ? 16 : f32 || of_item <= 64 ? 64 : 256;
+  // every item ends in a block of its own, not all of it filled
+  const int64_t blocks = (most <= s.rows ? 0 : n_rows * g / s.rows) + B;
+  const int64_t group_blocks = G > 0 ? n_rows * g / s.rows + G : 0;
+  s.blocks = (int)(blocks + group_blocks);
+  const int at_once = f32 ? (d == 128 ? 512 : 1024) : 256;                     // workgroups
+  s.round = std::max(at_once / Hkv, 1);
+  if (G > 0) {
+    s.slots = std::max(3 * s.round, s.blocks);
+  } else if (most <= s.rows) {
+    s.round = std::max(s.round, 2 * B);
+    // Requests of up to 512 tokens (fp32: 128) in one piece each and without a second pass, by what the tables hold.
+    s.slots = capacity <= (f32 ? 128 : 512) ? 0 : s.round;
+  } else {
+    // Cut where the blocks fill two thirds of the chip at most; two rounds of pieces if they end sooner.
+    const int64_t filled = (n_rows * g + s.rows - 1) / s.rows;
+    s.slots = 3 * filled <= 2 * s.round ? 2 * s.round : 0;
   }
-  if (b < 0 || i >= a.max_new) return;
-  const int64_t to = (int64_t)r * a.Hq + h;
-  const int pos = min(past + i, min(max(a.kv_len[b], 0), a.table_width << a.page_shift) - 1);
-  float q[kPer], o[kPer], m = kNothingSeen, l = 0.f;
-  for (int e = 0; e < kPer; ++e) {
-    q[e] = Elem<T>::load((const T *)a.q + r * a.q_row + (int64_t)h * kD + kPer * lane + e);
-    o[e] = 0.f;
-  }
-  for (int t = 0; t <= pos; ++t) {
-    const unsigned int page = min((unsigned int)a.block_table[b * a.table_stride + (t >> a.page_shift)], (unsigned int)(a.n_pages - 1));
-    const int token = t & ((1 << a.page_shift) - 1);
-    const int64_t at = page * a.stride_page + token * a.stride_token + c * a.stride_head + kPer * lane;
-    float k[kPer], v[kPer], s = 0.f;
-    for (int e = 0; e < kPer; ++e) {
-      if constexpr (std::is_same<C, e4m3_t>::value) {
-        const unsigned int bytes = ((const unsigned short *)a.exponents)[(((int64_t)page * a.Hkv + c) << a.page_shift) + token];
-        k[e] = __builtin_amdgcn_cvt_f32_fp8(((const e4m3_t *)a.k)[at + e], 0) * power_of(bytes & 0xffu);
-        v[e] = __builtin_amdgcn_cvt_f32_fp8(((const e4m3_t *)a.v)[at + e], 0) * power_of(bytes >> 8);
-      } else {
-        k[e] = Elem<C>::load((const C *)a.k + at + e);
-        v[e] = Elem<C>::load((const C *)a.v + at + e);
-      }
-      s = fmaf(q[e], k[e], s);
-    }
-    s = wave_sum(s);
-    const float m_new = fmaxf(m, s), alpha = factor(m, m_new, a.scale_log2), p = factor(s, m_new, a.scale_log2);
-    m = m_new;
-    l = fmaf(l, alpha, p);
-    for (int e = 0; e < kPer; ++e) o[e] = fmaf(o[e], alpha, p * v[e]);
-  }
-  for (int e = 0; e < kPer; ++e) Elem<T>::store((T *)a.out + to * kD + kPer * lane + e, pos < 0 ? 0.f : o[e] / l);
-  if (a.lse && lane == 0) a.lse[to] = pos < 0 ? -INFINITY : log_sum(m, a.scale_log2, l);
+  const int64_t units = (int64_t)s.slots * Hkv * s.rows;
+  s.floats_o = units * d;
+  s.floats_ml = units * 2;
+  return s;
 }
 
-template <typename T, typename C> hipError_t launch(int d, const ServeArgs &a, hipStream_t st) {
-  const dim3 grid(a.Hq, a.n_rows < 32768 ? a.n_rows : 32768, (a.n_rows + 32767) / 32768);
-  if (d == 128) hipLaunchKernelGGL((serve_attn_plain_kernel<T, C, 128>), grid, dim3(64), 0, st, a);
-  else hipLaunchKernelGGL((serve_attn_plain_kernel<T, C, 64>), grid, dim3(64), 0, st, a);
-  return hipGetLastError();
-}
-
-}  // namespace
-
-hipError_t launch_serve_attn(int dtype, int d, const ServeArgs &a, hipStream_t st) {
-  if (dtype == SPARROW_F32) return a.exponents ? launch<float, e4m3_t>(d, a, st) : launch<float, float>(d, a, st);
-  return a.exponents ? launch<bf16_t, e4m3_t>(d, a, st) : launch<bf16_t, bf16_t>(d, a, st);
+hipError_t launch_serve_attn(int dtype, int d, const ServeShape &s, const ServeArgs &a, hipStream_t st) {
+  const int blocks = std::max(s.blocks, s.slots);
+  const hipError_t e = dtype == SPARROW_F32 ? launch_serve_f32(d, blocks, a, st) : launch_serve_bf16(d, blocks, a, st);
+  if (e != hipSuccess || s.slots == 0) return e;
+  return launch_serve_combine(dtype, d, a, st);
 }
 
 }  // namespace sparrow

@@ -31,6 +31,7 @@ struct GatherArgs {
 };
 hipError_t launch_page_gather(int dtype, int d, const GatherArgs &a, hipStream_t st);
 
+struct ServeLeft;
 struct ServeArgs {
   const void *q, *k, *v;
   const uint8_t *exponents;
@@ -39,9 +40,19 @@ struct ServeArgs {
   float *lse;
   int64_t table_stride, q_row, stride_page, stride_token, stride_head;          // elements
   int32_t B, G, n_rows, max_new, Hq, Hkv, g, table_width, page_shift, n_pages;
-  float scale_log2;
+  int32_t block_shift;     // log2 of the rows of a block
+  int32_t slots, round;    // pieces per KV head at most (0: nothing is cut or shared, one piece a block); those that run at once
+  float scale_log2, inv_g;
+  float *part_o, *part_ml; // [piece * Hkv + KV head][row of the block]: unnormalised output [d]; reference score, sum
+  ServeLeft *left;         // [B]; NULL where slots is 0
 };
-hipError_t launch_serve_attn(int dtype, int d, const ServeArgs &a, hipStream_t st);
+// How a call of these sizes is run: rows per block, blocks per KV head at most, pieces, floats of part_o and part_ml.
+struct ServeShape {
+  int rows, blocks, slots, round;
+  int64_t floats_o, floats_ml;
+};
+ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t n_rows, int max_new, int64_t capacity);
+hipError_t launch_serve_attn(int dtype, int d, const ServeShape &s, const ServeArgs &a, hipStream_t st);
 
 // 2^(byte - 127) of a row of an 8-bit cache, normal and finite whatever the byte
 __device__ __forceinline__ float power_of(unsigned int byte) { return __uint_as_float(min(max(byte, 1u), 254u) << 23); }

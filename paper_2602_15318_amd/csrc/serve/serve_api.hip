@@ -21,7 +21,8 @@ int fail(int code, const char *fmt, ...) {
 }
 
 bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-int shift_of(int32_t page_size) { return 31 - __builtin_clz((unsigned)page_size); }
+size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+int shift_of(int32_t power) { return 31 - __builtin_clz((unsigned)power); }
 int64_t per_16_bytes(int32_t dtype) { return dtype == SPARROW_BF16 ? 8 : 4; }
 
 int check_table(int32_t B, int32_t page_size, int32_t table_width, int64_t table_stride) {
@@ -127,7 +128,13 @@ int attention(const sparrow_paged_desc *desc, const void *q, const void *k_cache
   a.g = desc->n_q_heads / desc->n_kv_heads;
   a.table_width = table_width; a.page_shift = shift_of(desc->page_size); a.n_pages = desc->n_pages;
   a.scale_log2 = (desc->scale > 0.f ? desc->scale : 1.0f / std::sqrt((float)desc->head_dim)) * kLog2e;
-  const hipError_t e = launch_serve_attn(desc->dtype, desc->head_dim, a, (hipStream_t)hip_stream);
+  a.inv_g = 1.0f / (float)a.g;
+  const ServeShape shape = serve_shape(desc->dtype, desc->head_dim, a.Hq, a.Hkv, B, n_groups, n_rows, max_new, (int64_t)table_width * desc->page_size);
+  a.slots = shape.slots; a.round = shape.round; a.block_shift = shift_of(shape.rows);
+  a.part_o = (float *)workspace;
+  a.part_ml = (float *)((unsigned char *)workspace + round_up((size_t)shape.floats_o * 4, 256));
+  a.left = shape.slots == 0 ? nullptr : (ServeLeft *)((unsigned char *)a.part_ml + round_up((size_t)shape.floats_ml * 4, 256));
+  const hipError_t e = launch_serve_attn(desc->dtype, desc->head_dim, shape, a, (hipStream_t)hip_stream);
   if (e != hipSuccess) return fail(SPARROW_ERR_DEVICE, "attention launch: %s", hipGetErrorString(e));
   return SPARROW_OK;
 }
@@ -203,7 +210,8 @@ int sparrow_page_gather(const sparrow_paged_desc *desc, const void *k_cache, con
 
 size_t sparrow_prefix_attn_workspace(const sparrow_paged_desc *desc, int32_t B, int32_t n_groups, int32_t n_rows, int32_t max_new) {
   if (!attention_sizes(desc, B, n_groups, n_rows, max_new)) return 0;
-  return 0;
+  const ServeShape s = serve_shape(desc->dtype, desc->head_dim, desc->n_q_heads, desc->n_kv_heads, B, n_groups, n_rows, max_new, SPARROW_MAX_PAGED_TOKENS);
+  return s.slots == 0 ? 0 : round_up((size_t)s.floats_o * 4, 256) + round_up((size_t)s.floats_ml * 4, 256) + round_up((size_t)B * 32, 256);
 }
 
 int sparrow_chunk_attn8(const sparrow_paged_desc *desc, const void *q, const void *k_cache, const void *v_cache,
