@@ -5,8 +5,9 @@
 
 namespace sparrow {
 
-hipError_t launch_serve_bf16(int d, int blocks, const ServeArgs &a, hipStream_t st);
-hipError_t launch_serve_f32(int d, int blocks, const ServeArgs &a, hipStream_t st);
+hipError_t launch_serve_plan(const ServeArgs &a, hipStream_t st);
+hipError_t launch_serve_bf16(int d, int pieces, const ServeArgs &a, hipStream_t st);
+hipError_t launch_serve_f32(int d, int pieces, const ServeArgs &a, hipStream_t st);
 hipError_t launch_serve_combine(int dtype, int d, const ServeArgs &a, hipStream_t st);
 
 ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t n_rows, int max_new, int64_t capacity) {
@@ -17,13 +18,11 @@ ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t 
   const int64_t of_item = G > 0 ? n_rows * g : most;                           // of an item
   s.rows = of_item <= 16 ? 16 : f32 || of_item <= 64 ? 64 : 256;
   // every item ends in a block of its own, not all of it filled
-  const int64_t blocks = (most <= s.rows ? 0 : n_rows * g / s.rows) + B;
-  const int64_t group_blocks = G > 0 ? n_rows * g / s.rows + G : 0;
-  s.blocks = (int)(blocks + group_blocks);
+  const int64_t blocks = (most <= s.rows ? 0 : n_rows * g / s.rows) + B + (G > 0 ? n_rows * g / s.rows + G : 0);
   const int at_once = f32 ? (d == 128 ? 512 : 1024) : 256;                     // workgroups
   s.round = std::max(at_once / Hkv, 1);
   if (G > 0) {
-    s.slots = std::max(3 * s.round, s.blocks);
+    s.slots = (int)std::max<int64_t>(4 * s.round, blocks);
   } else if (most <= s.rows) {
     s.round = std::max(s.round, 2 * B);
     // Requests of up to 512 tokens (fp32: 128) in one piece each and without a second pass, by what the tables hold.
@@ -33,6 +32,7 @@ ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t 
     const int64_t filled = (n_rows * g + s.rows - 1) / s.rows;
     s.slots = 3 * filled <= 2 * s.round ? 2 * s.round : 0;
   }
+  s.grid = (int)std::max<int64_t>(s.slots, G > 0 ? 0 : blocks);
   const int64_t units = (int64_t)s.slots * Hkv * s.rows;
   s.floats_o = units * d;
   s.floats_ml = units * 2;
@@ -40,8 +40,9 @@ ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t 
 }
 
 hipError_t launch_serve_attn(int dtype, int d, const ServeShape &s, const ServeArgs &a, hipStream_t st) {
-  const int blocks = std::max(s.blocks, s.slots);
-  const hipError_t e = dtype == SPARROW_F32 ? launch_serve_f32(d, blocks, a, st) : launch_serve_bf16(d, blocks, a, st);
+  hipError_t e = a.G > 0 ? launch_serve_plan(a, st) : hipSuccess;
+  if (e != hipSuccess) return e;
+  e = dtype == SPARROW_F32 ? launch_serve_f32(d, s.grid, a, st) : launch_serve_bf16(d, s.grid, a, st);
   if (e != hipSuccess || s.slots == 0) return e;
   return launch_serve_combine(dtype, d, a, st);
 }

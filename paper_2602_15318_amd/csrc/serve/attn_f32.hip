@@ -21,7 +21,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) serve_attn_f32_kernel(ServeArg
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = blockIdx.x, idx = blockIdx.y + 32768 * blockIdx.z;
   ServePiece pc;
-  if (!serve_find_piece(a, idx, lane, &pc)) return;   // uniform
+  if (!serve_piece(a, idx, &pc)) return;              // uniform
   const ServePages<C> pages = serve_pages<C>(a, pc.it, c);
   const int block_rows = 1 << a.block_shift, R = pc.it.n * a.g, rho0 = pc.block << a.block_shift;
   const int in_block = 16 * w + n16;
@@ -50,17 +50,17 @@ __global__ void __launch_bounds__(64 * kWaves, 2) serve_attn_f32_kernel(ServeArg
   typedef __attribute__((ext_vector_type(kD / 32))) unsigned int Codes;
   typedef __attribute__((ext_vector_type(2))) float f32x2;
   Codes kc, vc;
-  int powers = 0;
+  unsigned int powers = 0u;
   const auto fetch = [&](int tile) __attribute__((always_inline)) {
     const auto place = pages.place(pc.t0 + tile * kTokens + 8 * w);
     const unsigned int off = (lane / 8) * pages.stride_token + (kD / 8) * (lane % 8);
     kc = *(const Codes *)(pages.k + place.at + off);
     vc = *(const Codes *)(pages.v + place.at + off);
-    powers = pages.powers[place.token + lane / 8];
+    powers = pages.powers_of(place, lane / 8);
   };
   const auto store = [&](int buf) __attribute__((always_inline)) {
     unsigned char *to = lds + 2 * buf * kTileBytes + (8 * w + lane / 8) * kRow;
-    const float pk = power_of((unsigned int)powers & 0xffu), pv = power_of((unsigned int)powers >> 8);
+    const float pk = power_in(powers, lane / 8, false), pv = power_in(powers, lane / 8, true);
 #pragma unroll
     for (int i = 0; i < kD / 32; ++i) {                    // 16 bytes of fp32: four codes
       const int chunk = kD / 32 * (lane % 8) + i;
@@ -184,8 +184,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) serve_attn_f32_kernel(ServeArg
 
 }  // namespace
 
-hipError_t launch_serve_f32(int d, int blocks, const ServeArgs &a, hipStream_t st) {
-  const dim3 grid(a.Hkv, blocks < 32768 ? blocks : 32768, (blocks + 32767) / 32768), block(64 * kWaves);
+hipError_t launch_serve_f32(int d, int pieces, const ServeArgs &a, hipStream_t st) {
+  const dim3 grid(a.Hkv, pieces < 32768 ? pieces : 32768, (pieces + 32767) / 32768), block(64 * kWaves);
   if (a.exponents) {
     if (d == 128) hipLaunchKernelGGL((serve_attn_f32_kernel<e4m3_t, 128>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((serve_attn_f32_kernel<e4m3_t, 64>), grid, block, 0, st, a);

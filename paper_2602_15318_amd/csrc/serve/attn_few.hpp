@@ -2,8 +2,11 @@
 // keys; their states of a row are merged at the end.  As chunk_few16_kernel (../paged/chunk_attn_few16.hip), whose operands it has: S^T = K Q^T by
 // 16x16x32 products, P^T the scores' own registers, V^T by transposing reads.
 //
-// A bf16 cache's tiles go memory -> LDS past the registers, two tiles ahead.  An 8-bit cache's go through registers, kAhead tiles ahead, and are
-// written to LDS as the bf16 numbers that they are, so that scores and outputs see no powers.
+// Tiles go memory -> LDS past the registers, two tiles ahead.  An 8-bit cache's are tiles of 32 keys (the same bytes); their codes become bf16 numbers
+// in the operands, K's times its power, V's as they are: V's power multiplies the probability instead, which is exact too.  A 16-byte read of K gives
+// a lane its part of two k-steps (columns 16 x .. 16 x + 15 of chunk x, Q^T cut alike), a transposing read of bytes (ds_read_b64_tr_b8: within 16
+// lanes, lane i receives byte i % 8 of the 8-byte words addressed by lanes 2 j + i / 8, j = 0..7) V^T of eight keys.  (Products of 8-bit numbers, the
+// query as a sum of two e4m3 terms, take as many cycles and no conversion of K, but their sums were off by 2^-15 of the terms' sizes: 2^-24 in bf16.)
 #pragma once
 #include "serve_tiles.hpp"
 
@@ -12,191 +15,304 @@ namespace sparrow {
 constexpr int kServeWaves = 8;
 
 template <typename C, int kD> struct FewTiles {
-  static constexpr int kTokens = 16, kRow = 2 * kD, kTileBytes = kTokens * kRow, kBytes = kServeWaves * 4 * kTileBytes;
+  static constexpr bool k8 = std::is_same<C, e4m3_t>::value;
+  static constexpr int kTokens = k8 ? 32 : 16, kRow = kD * (int)sizeof(C), kTileBytes = kTokens * kRow;
+  static constexpr int kPowers = k8 ? 256 : 0;             // bytes of a tile's powers
+  static constexpr int kBytes = kServeWaves * (4 * kTileBytes + 2 * kPowers);       // [wave][K0, V0, K1, V1], [wave][powers 0, 1]
 };
 
-template <typename C, int kD>
-__device__ __forceinline__ void attend_few(const ServeArgs &a, const ServePiece &pc, int idx, int c, unsigned char *lds, float (*ml)[16][2]) {
-  constexpr bool k8 = std::is_same<C, e4m3_t>::value;
-  constexpr int kWaves = kServeWaves, kTokens = FewTiles<C, kD>::kTokens, kRow = FewTiles<C, kD>::kRow, kTileBytes = FewTiles<C, kD>::kTileBytes;
-  constexpr int kDB = kD / 16, kChunks = kRow / 16, kG = kRow / 64, kLoadRows = 64 / kChunks, kLoads = kTokens / kLoadRows, kOut = kD / 4;
-  constexpr int kAhead = 4, kCodes = kD / 64;              // 8 bits: tiles in flight; 16-byte loads of a tile
+// A wavefront's part of an item: its tiles w, w + 8, ... of the piece, its lane's row and what that has seen.
+struct FewPart {
+  int w, n, n_full, t0, t1, pos;     // tiles; those that all rows see whole; the piece's first token, last one seen + 1; the row's position
+  const bf16_t *q;                   // the row
+};
+template <int kD> struct FewState {
+  f32x4 o[kD / 16];
+  float m, l;
+  // The reference score moves only when a score of the wavefront's lies more than kSlack above it.
+  template <int kN> __device__ __forceinline__ void softmax(const f32x4 (&s)[kN], float (&p)[kN][4], float scale_log2) {
+    float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+#pragma unroll
+    for (int k = 1; k < kN; ++k) mx = fmaxf(mx, fmaxf(fmaxf(s[k][0], s[k][1]), fmaxf(s[k][2], s[k][3])));
+    if (__builtin_amdgcn_ballot_w64((mx - m) * scale_log2 > kSlack) != 0ull) {
+      const float m_new = fmaxf(m, quad_max(mx)), alpha = factor(m, m_new, scale_log2);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < kD / 16; ++db) o[db] *= alpha;
+    }
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[k][i] = fast_exp2((s[k][i] - m) * scale_log2);
+      l += (p[k][0] + p[k][1]) + (p[k][2] + p[k][3]);
+    }
+  }
+};
+
+template <int kD>
+__device__ __forceinline__ void few_of_bf16(const FewPart &x, const ServePages<bf16_t> &pages, float scale_log2, unsigned char *mine, FewState<kD> &st) {
+  constexpr int kWaves = kServeWaves, kTokens = 16, kRow = 2 * kD, kTileBytes = kTokens * kRow;
+  constexpr int kDB = kD / 16, kChunks = kRow / 16, kG = kRow / 64, kLoadRows = 64 / kChunks, kLoads = kTokens / kLoadRows;
   const int lane = threadIdx.x & 63, n16 = lane & 15, c4 = lane >> 4;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int R = pc.it.n * a.g;                             // (at most 16: one block)
-  const ServePages<C> pages = serve_pages<C>(a, pc.it, c);
-  const int last_pos = min(pc.it.past + quotient(R - 1, a.g), pc.it.to - 1), first_pos = pc.it.past;
-  const int t1 = min(pc.t1, last_pos + 1);
-  const int n_tiles = max(t1 - pc.t0 + kTokens - 1, 0) / kTokens;
-  const int n = (n_tiles - w + kWaves - 1) / kWaves;       // of this wavefront: w, w + kWaves, ...
-  unsigned char *mine = lds + w * 4 * kTileBytes;
   // Row r's 16-byte chunk x is kept at x ^ swz(r): eight rows read at one chunk, or four groups of four rows read transposed, fall on
   // different banks.
   const auto swz = [](int row) { return kRow == 128 ? ((row >> 1) & 3) << 1 : (row & 7) << 1; };
-
-  const int rho = min(n16, R - 1), i_row = quotient(rho, a.g, a.inv_g), pos = min(pc.it.past + i_row, pc.it.to - 1);
-  f32x4 o[kDB];
-  float m = kNothingSeen, l = 0.f;
+  const unsigned int mine_at = lds_offset(mine);
+  // load j of a tile: rows kLoadRows j + lane / kChunks
+  const auto issue = [&](const unsigned char *src, int it, int part) __attribute__((always_inline)) {
+    const unsigned char *at = src + pages.place(x.t0 + (x.w + it * kWaves) * kTokens).at;
 #pragma unroll
-  for (int db = 0; db < kDB; ++db) o[db] = (f32x4){0.f, 0.f, 0.f, 0.f};
-  if (n > 0) {
-    u32x4 q[kG];
-    const auto load_q = [&]() __attribute__((always_inline)) {
-      const bf16_t *at = (const bf16_t *)a.q + (int64_t)(pc.it.row0 + i_row) * a.q_row + (int64_t)(c * a.g + rho - i_row * a.g) * kD;
+    for (int j = 0; j < kLoads; ++j) {
+      const int row = kLoadRows * j + lane / kChunks;
+      global_to_lds<true>(at, row * pages.stride_token + 16u * ((lane % kChunks) ^ swz(row)), mine_at + part * kTileBytes + 1024 * j);
+    }
+  };
+  issue(pages.k, 0, 0);
+  issue(pages.v, 0, 1);
+  if (x.n > 1) {
+    issue(pages.k, 1, 2);
+    issue(pages.v, 1, 3);
+  }
+  u32x4 q[kG];
 #pragma unroll
-      for (int g = 0; g < kG; ++g) q[g] = ((const u32x4 *)at)[4 * g + c4];
-    };
-    // of the tile at K, from token t on: scores and softmax, then the output
-    float p[4], seen[4];
-    const auto scores = [&](const unsigned char *K, int t, auto masked) __attribute__((always_inline)) {
-      constexpr bool kMasked = decltype(masked)::value;
-      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  for (int g = 0; g < kG; ++g) q[g] = ((const u32x4 *)x.q)[4 * g + c4];
+  wait_loads<0>();
 #pragma unroll
-      for (int g = 0; g < kG; ++g) {
-        const u32x4 k = *reinterpret_cast<const u32x4 *>(K + n16 * kRow + (((4 * g + c4) ^ swz(n16)) << 4));
-        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[g]), s, 0, 0, 0);
-      }
-      if constexpr (kMasked) {
+  for (int g = 0; g < kG; ++g) asm volatile("" : "+v"(q[g]));              // (waited for here, and not in the loop)
+  const auto step = [&](int it, auto masked) __attribute__((always_inline)) {
+    constexpr bool kMasked = decltype(masked)::value;
+    const int buf = it & 1;
+    const bool more = it + 1 < x.n, more2 = it + 2 < x.n;
+    if (more) wait_loads<3 * kLoads>();
+    else wait_loads<kLoads>();
+    const unsigned char *K = mine + 2 * buf * kTileBytes, *V = K + kTileBytes;
+    f32x4 s[1] = {{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bool vis = t + 4 * c4 + i <= min(pos, t1 - 1);
-          s[i] = vis ? s[i] : -INFINITY;
-          seen[i] = vis ? 1.f : 0.f;
-        }
-      }
-      return s;
-    };
-    // the row's reference score moves only when a score of the wavefront's lies more than kSlack above it
-    const auto softmax = [&](f32x4 s) __attribute__((always_inline)) {
-      const float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-      if (__builtin_amdgcn_ballot_w64((mx - m) * a.scale_log2 > kSlack) != 0ull) {
-        const float m_new = fmaxf(m, quad_max(mx)), alpha = factor(m, m_new, a.scale_log2);
-        m = m_new;
-        l *= alpha;
-#pragma unroll
-        for (int db = 0; db < kDB; ++db) o[db] *= alpha;
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = fast_exp2((s[i] - m) * a.scale_log2);
-      l += (p[0] + p[1]) + (p[2] + p[3]);
-    };
-    const auto output = [&](const unsigned char *V, auto masked) __attribute__((always_inline)) {
-      constexpr bool kMasked = decltype(masked)::value;
-      const int row = 4 * c4 + (n16 >> 2);
-      bf16x4 v[kDB], pb, ones;
-#pragma unroll
-      for (int db = 0; db < kDB; ++db) v[db] = lds_tr(V + row * kRow + (((2 * db + ((n16 >> 1) & 1)) ^ swz(row)) << 4) + 8 * (n16 & 1));
+    for (int g = 0; g < kG; ++g) {
+      const u32x4 k = *reinterpret_cast<const u32x4 *>(K + n16 * kRow + (((4 * g + c4) ^ swz(n16)) << 4));
+      s[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[g]), s[0], 0, 0, 0);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more2) issue(pages.k, it + 2, 2 * buf);
+    const int t = x.t0 + (x.w + it * kWaves) * kTokens;
+    float p[1][4], seen[4];
+    if constexpr (kMasked) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        pb[i] = (__bf16)p[i];
-        if (kMasked) ones[i] = (__bf16)seen[i];
+        const bool vis = t + 4 * c4 + i <= min(x.pos, x.t1 - 1);
+        s[0][i] = vis ? s[0][i] : -INFINITY;
+        seen[i] = vis ? 1.f : 0.f;
       }
-      if constexpr (kMasked) {
-        add_masked16(v, pb, ones, o);
-      } else {
+    }
+    st.softmax(s, p, scale_log2);
+    if (more2) wait_loads<3 * kLoads>();
+    else if (more) wait_loads<2 * kLoads>();
+    else wait_loads<0>();
+    const int row = 4 * c4 + (n16 >> 2);
+    bf16x4 v[kDB], pb, ones;
 #pragma unroll
-        for (int db = 0; db < kDB; ++db) o[db] = mul16(v[db], pb, o[db]);
-      }
-    };
-    // the tiles that all rows see whole, then the others
-    const int full = max(min(first_pos + 1, t1) - pc.t0, 0) / kTokens, n_full = max(full - w + kWaves - 1, 0) / kWaves;
-    if constexpr (!k8) {
-      const unsigned int mine_at = lds_offset(mine);
-      // load j of a tile: rows kLoadRows j + lane / kChunks
-      const auto issue = [&](const unsigned char *src, int tile, int part) __attribute__((always_inline)) {
-        const unsigned char *at = src + pages.place(pc.t0 + tile * kTokens).at;
+    for (int db = 0; db < kDB; ++db) v[db] = lds_tr(V + row * kRow + (((2 * db + ((n16 >> 1) & 1)) ^ swz(row)) << 4) + 8 * (n16 & 1));
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-          const int row = kLoadRows * j + lane / kChunks;
-          global_to_lds<true>(at, row * pages.stride_token + 16u * ((lane % kChunks) ^ swz(row)), mine_at + part * kTileBytes + 1024 * j);
-        }
-      };
-      issue(pages.k, w, 0);
-      issue(pages.v, w, 1);
-      if (n > 1) {
-        issue(pages.k, w + kWaves, 2);
-        issue(pages.v, w + kWaves, 3);
-      }
-      load_q();
-      wait_loads<0>();
-      const auto step = [&](int it, auto masked) __attribute__((always_inline)) {
-        const int buf = it & 1;
-        const bool more = it + 1 < n, more2 = it + 2 < n;
-        if (more) wait_loads<3 * kLoads>();
-        else wait_loads<kLoads>();
-        const unsigned char *K = mine + 2 * buf * kTileBytes;
-        const f32x4 s = scores(K, pc.t0 + (w + it * kWaves) * kTokens, masked);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (more2) issue(pages.k, w + (it + 2) * kWaves, 2 * buf);
-        softmax(s);
-        if (more2) wait_loads<3 * kLoads>();
-        else if (more) wait_loads<2 * kLoads>();
-        else wait_loads<0>();
-        output(K + kTileBytes, masked);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (more2) issue(pages.v, w + (it + 2) * kWaves, 2 * buf + 1);
-      };
-      int it = 0;
-      for (; it < n_full; ++it) step(it, std::false_type());
-      for (; it < n; ++it) step(it, std::true_type());
+    for (int i = 0; i < 4; ++i) {
+      pb[i] = (__bf16)p[0][i];
+      if (kMasked) ones[i] = (__bf16)seen[i];
+    }
+    if constexpr (kMasked) {
+      add_masked16(v, pb, ones, st.o);
     } else {
-      // A lane has 16 codes of row kCodeRows j + lane / kCodeLanes, and that row's powers.
-      constexpr int kCodeLanes = kD / 16, kCodeRows = 64 / kCodeLanes;
-      u32x4 kc[kAhead][kCodes], vc[kAhead][kCodes];
-      unsigned short pw[kAhead][kCodes];
-      const auto fetch = [&](int tile, int u) __attribute__((always_inline)) {
-        const auto place = pages.place(pc.t0 + tile * kTokens);
 #pragma unroll
-        for (int j = 0; j < kCodes; ++j) {
-          const int row = kCodeRows * j + lane / kCodeLanes;
-          const unsigned int off = row * pages.stride_token + 16u * (lane % kCodeLanes);
-          kc[u][j] = __builtin_nontemporal_load((const u32x4 *)(pages.k + place.at + off));
-          vc[u][j] = __builtin_nontemporal_load((const u32x4 *)(pages.v + place.at + off));
-          pw[u][j] = pages.powers[place.token + row];
-        }
-      };
-      const auto store = [&](unsigned char *to, const u32x4 *codes, const unsigned short *powers, int shift) __attribute__((always_inline)) {
+      for (int db = 0; db < kDB; ++db) st.o[db] = mul16(v[db], pb, st.o[db]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more2) issue(pages.v, it + 2, 2 * buf + 1);
+  };
+  int it = 0;
+  for (; it < x.n_full; ++it) step(it, std::false_type());
+  for (; it < x.n; ++it) step(it, std::true_type());
+}
+
+__device__ __forceinline__ f32x4 mul32(bf16x8 v, bf16x8 p, f32x4 o) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o, 0, 0, 0); }
+// As add_masked16 (../paged/chunk_attn_16.hpp), of 32 keys.
+template <int kN> __device__ __forceinline__ void add_masked32(const bf16x8 (&v)[kN], bf16x8 p, bf16x8 seen, f32x4 *o) {
+  unsigned int any = 0u;
 #pragma unroll
-        for (int j = 0; j < kCodes; ++j) {
-          const int row = kCodeRows * j + lane / kCodeLanes;
-          const float power = power_of((powers[j] >> shift) & 0xffu);
+  for (int db = 0; db < kN; ++db)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const u32x2 x = four_of(codes[j][2 * h], power), y = four_of(codes[j][2 * h + 1], power);
-            *reinterpret_cast<u32x4 *>(to + row * kRow + (((2 * (lane % kCodeLanes) + h) ^ swz(row)) << 4)) = (u32x4){x[0], x[1], y[0], y[1]};
-          }
-        }
-      };
+    for (int i = 0; i < 4; ++i) any |= not_finite(__builtin_bit_cast(u32x4, v[db])[i]);
+  if (__builtin_amdgcn_ballot_w64(any != 0u) == 0ull) {
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (u < n) fetch(w + u * kWaves, u);
-      load_q();
-      const auto step = [&](int it, int u, auto masked) __attribute__((always_inline)) {
-        store(mine, kc[u], pw[u], 0);
-        store(mine + kTileBytes, vc[u], pw[u], 8);
-        if (it + kAhead < n) fetch(w + (it + kAhead) * kWaves, u);
-        asm volatile("" ::: "memory");
-        softmax(scores(mine, pc.t0 + (w + it * kWaves) * kTokens, masked));
-        output(mine + kTileBytes, masked);
-        asm volatile("" ::: "memory");
-      };
-      for (int it = 0; it < n; it += kAhead) {
+    for (int db = 0; db < kN; ++db) o[db] = mul32(v[db], p, o[db]);
+    return;
+  }
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          if (it + u < n_full) step(it + u, u, std::false_type());
-          else if (it + u < n) step(it + u, u, std::true_type());
+  for (int db = 0; db < kN; ++db) {
+    u32x4 fine = __builtin_bit_cast(u32x4, v[db]), up, down;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      up[i] = ones_of(fine[i], false);
+      down[i] = ones_of(fine[i], true);
+      fine[i] &= ~no_numbers(fine[i]);
+    }
+    o[db] = infinities(mul32(__builtin_bit_cast(bf16x8, fine), p, o[db]), mul32(__builtin_bit_cast(bf16x8, up), seen, zero),
+                       mul32(__builtin_bit_cast(bf16x8, down), seen, zero));
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+template <int kD>
+__device__ __forceinline__ void few_of_8bit(const FewPart &x, const ServePages<e4m3_t> &pages, float scale_log2, unsigned char *mine, unsigned char *powers,
+                                            FewState<kD> &st) {
+  constexpr int kWaves = kServeWaves, kTokens = 32, kRow = kD, kTileBytes = kTokens * kRow, kPowers = FewTiles<e4m3_t, kD>::kPowers;
+  constexpr int kDB = kD / 16, kChunks = kRow / 16, kLoadRows = 64 / kChunks, kLoads = kTokens / kLoadRows, kReads = kChunks / 4;
+  const int lane = threadIdx.x & 63, n16 = lane & 15, c4 = lane >> 4;
+  // Row r's 16-byte chunk x is kept at x ^ swz(r): eight rows of K read at one chunk, or of V at one chunk transposed (four of either half of the tile),
+  // fall on different banks.
+  const auto swz_k = [](int row) { return kD == 128 ? row & 7 : (row >> 2) & 1; };
+  const auto swz_v = [](int row) { return kD == 128 ? (row & 3) | ((row >> 4) & 1) << 2 : (row >> 4) & 1; };
+  const unsigned int mine_at = lds_offset(mine), powers_at = lds_offset(powers);
+  // load j of a tile: rows kLoadRows j + lane / kChunks; 16 tokens lie on one page
+  const auto token_of = [&](int it) __attribute__((always_inline)) { return x.t0 + (x.w + it * kWaves) * kTokens; };
+  const auto issue = [&](const unsigned char *src, const auto &swz, int it, int part) __attribute__((always_inline)) {
+    const unsigned char *at[2] = {src + pages.place(token_of(it)).at, src + pages.place(token_of(it) + 16).at};
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int row = kLoadRows * j + lane / kChunks;
+      global_to_lds<true>(at[kLoadRows * j / 16], (row & 15) * pages.stride_token + 16u * ((lane % kChunks) ^ swz(row)), mine_at + part * kTileBytes + 1024 * j);
+    }
+  };
+  const auto issue_k = [&](int it) __attribute__((always_inline)) {       // the powers of two tokens a lane, and K
+    const int64_t a = pages.place(token_of(it)).token, b = pages.place(token_of(it) + 16).token;
+    global_to_lds_4(pages.powers + 2 * ((lane & 8) ? b : a) + 4 * (lane & 7), powers_at + (it & 1) * kPowers);
+    issue(pages.k, swz_k, it, 2 * (it & 1));
+  };
+  const auto issue_v = [&](int it) __attribute__((always_inline)) { issue(pages.v, swz_v, it, 2 * (it & 1) + 1); };
+  issue_k(0);
+  issue_v(0);
+  if (x.n > 1) {
+    issue_k(1);
+    issue_v(1);
+  }
+  bf16x8 q[kReads][2];
+#pragma unroll
+  for (int g = 0; g < kReads; ++g)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) q[g][i] = ((const bf16x8 *)x.q)[2 * (4 * g + c4) + i];
+  wait_loads<0>();
+#pragma unroll
+  for (int g = 0; g < kReads; ++g) asm volatile("" : "+v"(q[g][0]), "+v"(q[g][1]));      // (waited for here, and not in the loop)
+  const auto step = [&](int it, auto masked) __attribute__((always_inline)) {
+    constexpr bool kMasked = decltype(masked)::value;
+    const int buf = it & 1;
+    const bool more = it + 1 < x.n, more2 = it + 2 < x.n;
+    if (more) wait_loads<3 * kLoads + 1>();
+    else wait_loads<kLoads>();
+    const unsigned char *K = mine + 2 * buf * kTileBytes, *V = K + kTileBytes, *P = powers + buf * kPowers;
+    f32x4 s[2];
+    u32x2 pv[2];                                           // K's and V's bytes of tokens 4 c4 + 0..3 of either half
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      pv[k] = *reinterpret_cast<const u32x2 *>(P + 32 * k + 8 * c4);
+      const int row = 16 * k + n16;
+      const float power = power_of(P[2 * row]);
+      s[k] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int g = 0; g < kReads; ++g) {
+        const u32x4 codes = *reinterpret_cast<const u32x4 *>(K + row * kRow + (((4 * g + c4) ^ swz_k(row)) << 4));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const u32x2 lo = four_of(codes[2 * i], power), hi = four_of(codes[2 * i + 1], power);
+          s[k] = mul32(__builtin_bit_cast(bf16x8, (u32x4){lo[0], lo[1], hi[0], hi[1]}), q[g][i], s[k]);
         }
       }
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more2) issue_k(it + 2);
+    float p[2][4], seen[2][4];
+    if constexpr (kMasked) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool vis = token_of(it) + 16 * k + 4 * c4 + i <= min(x.pos, x.t1 - 1);
+          s[k][i] = vis ? s[k][i] : -INFINITY;
+          seen[k][i] = vis ? 1.f : 0.f;
+        }
+    }
+    st.softmax(s, p, scale_log2);
+    bf16x8 pb, ones;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        pb[4 * k + i] = (__bf16)(p[k][i] * power_in(pv[k][i >> 1], i, true));
+        if (kMasked) ones[4 * k + i] = (__bf16)seen[k][i];
+      }
+    if (more2) wait_loads<3 * kLoads + 2>();
+    else if (more) wait_loads<2 * kLoads + 1>();
+    else wait_loads<0>();
+    const int j = n16 >> 1, row = 4 * c4 + (j & 3) + 16 * (j >> 2);
+    bf16x8 v[kDB];
+#pragma unroll
+    for (int db = 0; db < kDB; ++db) {
+      typedef __attribute__((ext_vector_type(2))) int i32x2;
+      const i32x2 codes = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(V + row * kRow + ((db ^ swz_v(row)) << 4) + 8 * (n16 & 1)));
+      const u32x2 lo = four_of((unsigned int)codes[0], 1.f), hi = four_of((unsigned int)codes[1], 1.f);
+      v[db] = __builtin_bit_cast(bf16x8, (u32x4){lo[0], lo[1], hi[0], hi[1]});
+    }
+    if constexpr (kMasked) {
+      add_masked32(v, pb, ones, st.o);
+    } else {
+#pragma unroll
+      for (int db = 0; db < kDB; ++db) st.o[db] = mul32(v[db], pb, st.o[db]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more2) issue_v(it + 2);
+  };
+  int it = 0;
+  for (; it < x.n_full; ++it) step(it, std::false_type());
+  for (; it < x.n; ++it) step(it, std::true_type());
+}
+
+template <typename C, int kD>
+__device__ __forceinline__ void attend_few(const ServeArgs &a, const ServePiece &pc, int idx, int c, unsigned char *lds, float (*ml)[16][2]) {
+  using Tiles = FewTiles<C, kD>;
+  constexpr int kWaves = kServeWaves, kTokens = Tiles::kTokens, kDB = kD / 16, kOut = kD / 4;
+  const int lane = threadIdx.x & 63, n16 = lane & 15, c4 = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int R = pc.it.n * a.g;                             // (at most 16: one block)
+  const int rho = min(n16, R - 1), i_row = quotient(rho, a.g, a.inv_g);
+  const int last_pos = min(pc.it.past + quotient(R - 1, a.g), pc.it.to - 1);
+  FewPart x;
+  x.w = w;
+  x.t0 = pc.t0;
+  x.t1 = min(pc.t1, last_pos + 1);
+  x.pos = min(pc.it.past + i_row, pc.it.to - 1);
+  x.q = (const bf16_t *)a.q + (int64_t)(pc.it.row0 + i_row) * a.q_row + (int64_t)(c * a.g + rho - i_row * a.g) * kD;
+  const int n_tiles = max(x.t1 - x.t0 + kTokens - 1, 0) / kTokens;
+  x.n = (n_tiles - w + kWaves - 1) / kWaves;
+  const int full = max(min(pc.it.past + 1, x.t1) - x.t0, 0) / kTokens;
+  x.n_full = max(full - w + kWaves - 1, 0) / kWaves;
+  FewState<kD> st;
+  st.m = kNothingSeen;
+  st.l = 0.f;
+#pragma unroll
+  for (int db = 0; db < kDB; ++db) st.o[db] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  if (x.n > 0) {
+    const ServePages<C> pages = serve_pages<C>(a, pc.it, c);
+    unsigned char *mine = lds + w * 4 * Tiles::kTileBytes;
+    if constexpr (Tiles::k8) few_of_8bit<kD>(x, pages, a.scale_log2, mine, lds + kWaves * 4 * Tiles::kTileBytes + w * 2 * Tiles::kPowers, st);
+    else few_of_bf16<kD>(x, pages, a.scale_log2, mine, st);
   }
   // ---- merge: states of the wavefronts through LDS
   __syncthreads();
   unsigned char *states = lds + w * 16 * kD * 4;
-  l = quad_sum(l);
-  if (c4 == 0) { ml[w][n16][0] = m; ml[w][n16][1] = l; }
+  const float l = quad_sum(st.l);
+  if (c4 == 0) { ml[w][n16][0] = st.m; ml[w][n16][1] = l; }
 #pragma unroll
   for (int db = 0; db < kDB; ++db)                         // elements 16 db + 4 c4 + 0..3
-    *reinterpret_cast<f32x4 *>(states + (n16 * kOut + ((4 * db + c4) ^ n16)) * 16) = o[db];
+    *reinterpret_cast<f32x4 *>(states + (n16 * kOut + ((4 * db + c4) ^ n16)) * 16) = st.o[db];
   __syncthreads();
   if (!pc.direct && idx >= a.slots) return;                // (offsets that overlap)
   const int64_t part = ((int64_t)idx * a.Hkv + c) << a.block_shift;

@@ -2,8 +2,8 @@
 // the workgroup shares.  As chunk_many_kernel (../paged/chunk_attn_many.hip): wavefronts w and w + 4 share a SIMD and run half a step apart, one in
 // the products of a step (scores of a tile, output of the tile before) while the other is in its softmax; four tiles of K and of V in LDS.
 //
-// A bf16 cache's tiles go memory -> LDS past the registers.  An 8-bit cache's are asked for a step ahead into registers, made the bf16 numbers
-// that they are in the softmax's half step, 1/8 by each wavefront, and written to LDS.
+// A bf16 cache's tiles go memory -> LDS past the registers.  An 8-bit cache's are asked for a step ahead into registers, made the bf16 numbers that they
+// are in the softmax's half step, 1/8 by each wavefront, and written to LDS.
 //
 // Probabilities are rounded to bf16 for the output's product, half a step 2^-9 to 2^-8 of a term; the row's sum takes them unrounded.
 #pragma once
@@ -12,13 +12,15 @@
 namespace sparrow {
 
 template <int kD> struct ManyTiles {
-  static constexpr int kTokens = 64, kStages = 4, kTileBytes = kTokens * 2 * kD, kBytes = 2 * kStages * kTileBytes;
+  static constexpr int kTokens = 64, kStages = 4, kTileBytes = kTokens * kD * 2;
+  static constexpr int kBytes = 2 * kStages * kTileBytes;  // K tiles, V tiles
 };
 
 template <typename C, int kD>
 __device__ __forceinline__ void attend_many(const ServeArgs &a, const ServePiece &pc, int idx, int c, unsigned char *lds) {
   constexpr bool k8 = std::is_same<C, e4m3_t>::value;
-  constexpr int kTokens = ManyTiles<kD>::kTokens, kStages = ManyTiles<kD>::kStages, kTileBytes = ManyTiles<kD>::kTileBytes;
+  using Tiles = ManyTiles<kD>;
+  constexpr int kTokens = Tiles::kTokens, kStages = Tiles::kStages, kTileBytes = Tiles::kTileBytes;
   constexpr int kDB = kD / 32, kKS = kD / 16, kHalf = kKS / 2;
   // The requests in the half step that has time left, the vector one with heads of 128, the matrix one with heads of 64.
   constexpr bool kLate = kD == 128;
@@ -53,6 +55,7 @@ __device__ __forceinline__ void attend_many(const ServeArgs &a, const ServePiece
   if (n > 0) {
     const auto place = [&](int tile) __attribute__((always_inline)) { return pages.place(pc.t0 + min(tile, n - 1) * kTokens + 8 * w); };
     using Place = typename ServePages<C>::Place;
+    const auto stage = [&](int t) { return t & (kStages - 1); };
     // ---- bf16: straight to LDS
     const unsigned int lds0 = lds_offset(lds) + 1024 * kLoads * w;
     unsigned int from_k[kLoads], from_v[kLoads];
@@ -66,22 +69,21 @@ __device__ __forceinline__ void attend_many(const ServeArgs &a, const ServePiece
     }
     const auto load_k = [&](Place at, int t) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) global_to_lds<false>(pages.k + at.at, from_k[j], lds0 + (t & (kStages - 1)) * kTileBytes + 1024 * j);
+      for (int j = 0; j < kLoads; ++j) global_to_lds<false>(pages.k + at.at, from_k[j], lds0 + stage(t) * kTileBytes + 1024 * j);
     };
     const auto load_v = [&](Place at, int t) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j)
-        global_to_lds<false>(pages.v + at.at, from_v[j], lds0 + (kStages + (t & (kStages - 1))) * kTileBytes + 1024 * j);
+      for (int j = 0; j < kLoads; ++j) global_to_lds<false>(pages.v + at.at, from_v[j], lds0 + (kStages + stage(t)) * kTileBytes + 1024 * j);
     };
-    // ---- 8 bits: kD / 8 codes of row 8 w + lane / 8, and that row's power
+    // ---- 8 bits: kD / 8 codes of row 8 w + lane / 8
     typedef __attribute__((ext_vector_type(kD / 32))) unsigned int Codes;
     const int row = 8 * w + lane / 8;
     const unsigned int off = (lane / 8) * pages.stride_token + (kD / 8) * (lane % 8);
     const auto fetch = [&](const unsigned char *src, Place at) __attribute__((always_inline)) { return *(const Codes *)(src + at.at + off); };
-    const auto power = [&](Place at, int shift) __attribute__((always_inline)) { return (pages.powers[at.token + lane / 8] >> shift) & 0xff; };
-    const auto store = [&](Codes x, int byte, bool is_v, int t) __attribute__((always_inline)) {
-      const float p = power_of((unsigned int)byte);
-      unsigned char *to = lds + ((is_v ? kStages : 0) + (t & (kStages - 1))) * kTileBytes;
+    const auto powers = [&](Place at) __attribute__((always_inline)) { return pages.powers_of(at, lane / 8); };
+    const auto store = [&](Codes x, unsigned int bytes, bool is_v, int t) __attribute__((always_inline)) {
+      const float p = power_in(bytes, lane / 8, is_v);
+      unsigned char *to = lds + ((is_v ? kStages : 0) + stage(t)) * kTileBytes;
 #pragma unroll
       for (int i = 0; i < kD / 64; ++i) {                  // 16 bytes of bf16: eight codes
         const u32x2 y = four_of(x[2 * i], p), z = four_of(x[2 * i + 1], p);
@@ -90,7 +92,7 @@ __device__ __forceinline__ void attend_many(const ServeArgs &a, const ServePiece
       }
     };
     Codes kc, vc;
-    int kp = 0, vp = 0;
+    unsigned int kp = 0u, vp = 0u;
 
     const Place p0 = place(0), p1 = place(1), p2 = place(2);
     if constexpr (!k8) {
@@ -100,18 +102,19 @@ __device__ __forceinline__ void attend_many(const ServeArgs &a, const ServePiece
       load_v(p1, 1);
       load_k(p2, 2);
     } else {
-      const Codes k0 = fetch(pages.k, p0), v0 = fetch(pages.v, p0), k1 = fetch(pages.k, p1), v1 = fetch(pages.v, p1), k2 = fetch(pages.k, p2);
-      const int b0 = power(p0, 0), c0 = power(p0, 8), b1 = power(p1, 0), c1 = power(p1, 8), b2 = power(p2, 0);
+      const Codes k0 = fetch(pages.k, p0), v0 = fetch(pages.v, p0), k1 = fetch(pages.k, p1), v1 = fetch(pages.v, p1);
+      const Codes k2 = fetch(pages.k, p2);
+      const unsigned int b0 = powers(p0), b1 = powers(p1);
+      vc = fetch(pages.v, p2);
+      vp = powers(p2);
       const Place p3 = place(3);
       kc = fetch(pages.k, p3);
-      kp = power(p3, 0);
-      vc = fetch(pages.v, p2);
-      vp = power(p2, 8);
+      kp = powers(p3);
       store(k0, b0, false, 0);
-      store(v0, c0, true, 0);
+      store(v0, b0, true, 0);
       store(k1, b1, false, 1);
-      store(v1, c1, true, 1);
-      store(k2, b2, false, 2);
+      store(v1, b1, true, 1);
+      store(k2, vp, false, 2);
     }
     bf16x8 q[kKS];
     {
@@ -119,11 +122,11 @@ __device__ __forceinline__ void attend_many(const ServeArgs &a, const ServePiece
 #pragma unroll
       for (int ks = 0; ks < kKS; ++ks) q[ks] = *(const bf16x8 *)(at + 32 * ks);
     }
-    // Half steps of tile t: A(t), its scores (and the output of tile t - 1), then B(t), its softmax; a barrier ends each.  K of tile t + 3 and V of
-    // t + 2, whose places A(t - 1) was the last to read, are asked for in A(t) or B(t) (bf16), or written in B(t), asked for in B(t - 1) (8 bits).
-    // K of t + 2 and V of t + 1 are there before either half of the workgroup begins A(t + 1): a wavefront ends B(t) when all but the bf16 requests
-    // of this step are done.
-    Place at_v = p2, at_k = place(3);
+    // Half steps of tile t: A(t), its scores (and the output of tile t - 1), then B(t), its softmax; a barrier ends each.  A(t) or B(t) asks for K of
+    // tile t + 3 and V of t + 2, whose places A(t - 1) was the last to read; a wavefront ends B(t) when all but its last requests are done, those of this
+    // step: K of t + 2 and V of t + 1 are there before either half of the workgroup begins A(t + 1).  8 bits: B(t) writes K of t + 3 and V of t + 2,
+    // asked for in B(t - 1), and asks for their successors.
+    Place at_v = k8 ? place(3) : p2, at_k = place(k8 ? 4 : 3);
     if constexpr (!k8) wait_loads<0>();
     barrier();
     if (w >= 4) barrier();                                 // half a step behind
@@ -139,18 +142,23 @@ __device__ __forceinline__ void attend_many(const ServeArgs &a, const ServePiece
         if (kLate) request(t);
         at_v = at_k;
         at_k = place(t + 4);
-      } else {
-        store(kc, kp, false, t + 3);
-        store(vc, vp, true, t + 2);
-        vc = fetch(pages.v, at_k);
-        vp = power(at_k, 8);
-        at_k = place(t + 4);
-        kc = fetch(pages.k, at_k);
-        kp = power(at_k, 0);
       }
     };
-    const auto end_b = [&]() __attribute__((always_inline)) {
-      if constexpr (!k8) wait_loads<2 * kLoads>();
+    // (8 bits behind the softmax: before it the chunk of 2,048 tokens over 26,112 takes 781 us instead of 685)
+    const auto end_b = [&](int t) __attribute__((always_inline)) {
+      if constexpr (!k8) {
+        wait_loads<2 * kLoads>();
+      } else {
+        asm volatile("" : "+v"(kp), "+v"(vp));             // (what is made of them is made here: earlier, the loads would be waited for earlier)
+        store(kc, kp, false, t + 3);
+        store(vc, vp, true, t + 2);
+        vc = fetch(pages.v, at_v);
+        vp = kp;
+        kc = fetch(pages.k, at_k);
+        kp = powers(at_k);
+        at_v = at_k;
+        at_k = place(t + 5);
+      }
       barrier();
     };
     if (!have) {
@@ -158,7 +166,7 @@ __device__ __forceinline__ void attend_many(const ServeArgs &a, const ServePiece
       barrier();
       for (int t = 0; t < n; ++t) {
         begin_b(t);
-        end_b();
+        end_b(t);
         begin_a(t + 1);
         barrier();
       }
@@ -166,7 +174,7 @@ __device__ __forceinline__ void attend_many(const ServeArgs &a, const ServePiece
       f32x16 s[2];
       bf16x8 pb[4], kf[2][kHalf];                          // kf: the first half of the columns of the next tile's K
       const auto tile = [&](int t, int stage0, int at) __attribute__((always_inline)) {
-        at += (stage0 + (t & (kStages - 1))) * kTileBytes;
+        at += (stage0 + stage(t)) * kTileBytes;
         asm volatile("" : "+v"(at));                       // (worked out here: kept, the offsets cost more registers than there are)
         return at;
       };
@@ -230,35 +238,31 @@ __device__ __forceinline__ void attend_many(const ServeArgs &a, const ServePiece
         for (int st = 0; st < 4; ++st) pb[st] = __builtin_bit_cast(bf16x8, pw[st]);
       };
       const int k0 = k_at<kD>(lane), v0 = vt_at<kD>(lane);
-      const auto scores = [&](int t) __attribute__((always_inline)) {       // from kf on
+      // the scores of tile t, the first half of whose K is there; `then` between the two
+      const auto scores = [&](int t, auto then) __attribute__((always_inline)) {
         bf16x8 k2[2][kHalf];
         read_k(tile(t, 0, k0), kHalf, k2);
         s[0] = s[1] = (f32x16){0.f};
         __builtin_amdgcn_sched_barrier(0);
         multiply(0, kf);
         __builtin_amdgcn_sched_barrier(0);
+        then();
         multiply(kHalf, k2);
       };
       read_k(tile(0, 0, k0), 0, kf);
       begin_a(0);
-      scores(0);
+      scores(0, [] {});
       barrier();
       int t = 0;
       for (; t < n_full; ++t) {
         read_k(tile(t + 1, 0, k0), 0, kf);                 // (behind the last tile: of one that nothing is done with)
         begin_b(t);
         softmax();
-        end_b();
+        end_b(t);
         begin_a(t + 1);
         const int vt = tile(t, kStages, v0);
-        bf16x8 k2[2][kHalf], v[2][4];
-        read_k(tile(t + 1, 0, k0), kHalf, k2);
-        s[0] = s[1] = (f32x16){0.f};
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(0, kf);
-        __builtin_amdgcn_sched_barrier(0);
-        read_v(vt, 0, v[0]);
-        multiply(kHalf, k2);
+        bf16x8 v[2][4];
+        scores(t + 1, [&]() __attribute__((always_inline)) { read_v(vt, 0, v[0]); });
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int db = 0; db < kDB; ++db) {
@@ -290,9 +294,9 @@ __device__ __forceinline__ void attend_many(const ServeArgs &a, const ServePiece
           __builtin_amdgcn_sched_barrier(0);
         }
         read_k(tile(t + 1, 0, k0), 0, kf);
-        end_b();
+        end_b(t);
         begin_a(t + 1);
-        scores(t + 1);
+        scores(t + 1, [] {});
         barrier();
       }
     }

@@ -32,6 +32,7 @@ struct GatherArgs {
 hipError_t launch_page_gather(int dtype, int d, const GatherArgs &a, hipStream_t st);
 
 struct ServeLeft;
+struct ServePiece;
 struct ServeArgs {
   const void *q, *k, *v;
   const uint8_t *exponents;
@@ -45,10 +46,12 @@ struct ServeArgs {
   float scale_log2, inv_g;
   float *part_o, *part_ml; // [piece * Hkv + KV head][row of the block]: unnormalised output [d]; reference score, sum
   ServeLeft *left;         // [B]; NULL where slots is 0
+  ServePiece *pieces;      // with groups: [slots], n_pieces of them
+  int32_t *n_pieces;
 };
-// How a call of these sizes is run: rows per block, blocks per KV head at most, pieces, floats of part_o and part_ml.
+// How a call of these sizes is run: rows per block, pieces per KV head at most, those that run at once, workgroups per KV head, floats of part_o and part_ml.
 struct ServeShape {
-  int rows, blocks, slots, round;
+  int rows, slots, round, grid;
   int64_t floats_o, floats_ml;
 };
 ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t n_rows, int max_new, int64_t capacity);

@@ -134,6 +134,8 @@ int attention(const sparrow_paged_desc *desc, const void *q, const void *k_cache
   a.part_o = (float *)workspace;
   a.part_ml = (float *)((unsigned char *)workspace + round_up((size_t)shape.floats_o * 4, 256));
   a.left = shape.slots == 0 ? nullptr : (ServeLeft *)((unsigned char *)a.part_ml + round_up((size_t)shape.floats_ml * 4, 256));
+  a.n_pieces = n_groups == 0 ? nullptr : (int32_t *)((unsigned char *)a.left + round_up((size_t)B * 32, 256));
+  a.pieces = n_groups == 0 ? nullptr : (ServePiece *)((unsigned char *)a.n_pieces + 256);
   const hipError_t e = launch_serve_attn(desc->dtype, desc->head_dim, shape, a, (hipStream_t)hip_stream);
   if (e != hipSuccess) return fail(SPARROW_ERR_DEVICE, "attention launch: %s", hipGetErrorString(e));
   return SPARROW_OK;
@@ -211,7 +213,8 @@ int sparrow_page_gather(const sparrow_paged_desc *desc, const void *k_cache, con
 size_t sparrow_prefix_attn_workspace(const sparrow_paged_desc *desc, int32_t B, int32_t n_groups, int32_t n_rows, int32_t max_new) {
   if (!attention_sizes(desc, B, n_groups, n_rows, max_new)) return 0;
   const ServeShape s = serve_shape(desc->dtype, desc->head_dim, desc->n_q_heads, desc->n_kv_heads, B, n_groups, n_rows, max_new, SPARROW_MAX_PAGED_TOKENS);
-  return s.slots == 0 ? 0 : round_up((size_t)s.floats_o * 4, 256) + round_up((size_t)s.floats_ml * 4, 256) + round_up((size_t)B * 32, 256);
+  return s.slots == 0 ? 0 : round_up((size_t)s.floats_o * 4, 256) + round_up((size_t)s.floats_ml * 4, 256) + round_up((size_t)B * 32, 256) +
+                                (n_groups == 0 ? 0 : 256 + round_up((size_t)s.slots * 48, 256));
 }
 
 int sparrow_chunk_attn8(const sparrow_paged_desc *desc, const void *q, const void *k_cache, const void *v_cache,

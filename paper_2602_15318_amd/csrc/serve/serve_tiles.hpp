@@ -11,7 +11,7 @@ namespace sparrow {
 template <typename C> struct ServePages {
   const int32_t __attribute__((address_space(4))) *table;     // read through the scalar cache
   const unsigned char *k, *v;                                  // the head's first row
-  const unsigned short *powers;                                // the head's first token, K's byte below V's
+  const unsigned char *powers;                                 // the head's first token, K's byte below V's
   int64_t stride_page, powers_page;                            // bytes; tokens
   unsigned int stride_token;
   int shift, last;                                             // last page entry that the item holds
@@ -22,13 +22,15 @@ template <typename C> struct ServePages {
     const int row = t & ((1 << shift) - 1);
     return {(int64_t)page * stride_page + (int64_t)row * stride_token, (int64_t)page * powers_page + row};
   }
+  // The bytes of row `row` (and of its neighbour, four in all) of rows that begin at an even token
+  __device__ __forceinline__ unsigned int powers_of(Place at, int row) const { return *(const unsigned int *)(powers + 2 * at.token + 2 * (row & ~1)); }
 };
 template <typename C> __device__ __forceinline__ ServePages<C> serve_pages(const ServeArgs &a, const ServeItem &it, int c) {
   ServePages<C> p;
   p.table = (const int32_t __attribute__((address_space(4))) *)(uintptr_t)(a.block_table + (int64_t)it.table * a.table_stride);
   p.k = (const unsigned char *)((const C *)a.k + (int64_t)c * a.stride_head);
   p.v = (const unsigned char *)((const C *)a.v + (int64_t)c * a.stride_head);
-  p.powers = (const unsigned short *)a.exponents + ((int64_t)c << a.page_shift);
+  p.powers = a.exponents + 2 * ((int64_t)c << a.page_shift);
   p.stride_page = (int64_t)sizeof(C) * a.stride_page;
   p.powers_page = (int64_t)a.Hkv << a.page_shift;
   p.stride_token = (unsigned int)(sizeof(C) * a.stride_token);
@@ -38,10 +40,19 @@ template <typename C> __device__ __forceinline__ ServePages<C> serve_pages(const
   return p;
 }
 
+// K's, or V's, power of row `row` from the four bytes of it and its neighbour
+__device__ __forceinline__ float power_in(unsigned int bytes, int row, bool is_v) {
+  return power_of((bytes >> (16 * (row & 1) + (is_v ? 8 : 0))) & 0xffu);
+}
 // Four codes times a power of two, exactly, as four bf16
 __device__ __forceinline__ u32x2 four_of(unsigned int codes, float power) {
   return (u32x2){__builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, power, false)),
                  __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, power, true))};
+}
+
+// 4 bytes per lane, each from an address of its own, to LDS: lane l's at dst + 4 l
+__device__ __forceinline__ void global_to_lds_4(const void *at, unsigned int dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(at) : "memory", "m0");
 }
 
 }  // namespace sparrow
