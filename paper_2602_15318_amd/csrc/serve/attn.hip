@@ -6,7 +6,7 @@
 namespace sparrow {
 
 hipError_t launch_serve_plan(const ServeArgs &a, hipStream_t st);
-hipError_t launch_serve_bf16(int d, int pieces, const ServeArgs &a, hipStream_t st);
+hipError_t launch_serve_bf16(int d, const ServeShape &s, const ServeArgs &a, hipStream_t st);
 hipError_t launch_serve_f32(int d, int pieces, const ServeArgs &a, hipStream_t st);
 hipError_t launch_serve_combine(int dtype, int d, const ServeArgs &a, hipStream_t st);
 
@@ -19,7 +19,9 @@ ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t 
   s.rows = of_item <= 16 ? 16 : f32 || of_item <= 64 ? 64 : 256;
   // every item ends in a block of its own, not all of it filled
   const int64_t blocks = (most <= s.rows ? 0 : n_rows * g / s.rows) + B + (G > 0 ? n_rows * g / s.rows + G : 0);
-  const int at_once = f32 ? (d == 128 ? 512 : 1024) : 256;                     // workgroups
+  // Single tokens: the fewer (request, KV head) pairs, the fewer and larger the workgroups, and the fewer pieces there are to put together.
+  s.waves = B * Hkv <= 48 ? 8 : B * Hkv < 192 ? 4 : 2;
+  const int at_once = f32 ? (d == 128 ? 512 : 1024) : G == 0 && s.rows == 16 ? 2048 / s.waves : 256;       // workgroups
   s.round = std::max(at_once / Hkv, 1);
   if (G > 0) {
     s.slots = (int)std::max<int64_t>(4 * s.round, blocks);
@@ -42,7 +44,7 @@ ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t 
 hipError_t launch_serve_attn(int dtype, int d, const ServeShape &s, const ServeArgs &a, hipStream_t st) {
   hipError_t e = a.G > 0 ? launch_serve_plan(a, st) : hipSuccess;
   if (e != hipSuccess) return e;
-  e = dtype == SPARROW_F32 ? launch_serve_f32(d, s.grid, a, st) : launch_serve_bf16(d, s.grid, a, st);
+  e = dtype == SPARROW_F32 ? launch_serve_f32(d, s.grid, a, st) : launch_serve_bf16(d, s, a, st);
   if (e != hipSuccess || s.slots == 0) return e;
   return launch_serve_combine(dtype, d, a, st);
 }

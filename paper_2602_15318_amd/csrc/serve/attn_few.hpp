@@ -1,4 +1,4 @@
-// Attention of up to 16 rows (new token, query head of the group) of an item by a workgroup of eight wavefronts, each with every eighth tile of 16
+// Attention of up to 16 rows (new token, query head of the group) of an item by a workgroup of kWaves wavefronts, each with every kWaves-th tile of 16
 // keys; their states of a row are merged at the end.  As chunk_few16_kernel (../paged/chunk_attn_few16.hip), whose operands it has: S^T = K Q^T by
 // 16x16x32 products, P^T the scores' own registers, V^T by transposing reads.
 //
@@ -12,16 +12,16 @@
 
 namespace sparrow {
 
-constexpr int kServeWaves = 8;
-
-template <typename C, int kD> struct FewTiles {
+template <typename C, int kD, int kWaves> struct FewTiles {
   static constexpr bool k8 = std::is_same<C, e4m3_t>::value;
   static constexpr int kTokens = k8 ? 32 : 16, kRow = kD * (int)sizeof(C), kTileBytes = kTokens * kRow;
   static constexpr int kPowers = k8 ? 256 : 0;             // bytes of a tile's powers
-  static constexpr int kBytes = kServeWaves * (4 * kTileBytes + 2 * kPowers);       // [wave][K0, V0, K1, V1], [wave][powers 0, 1]
+  static constexpr int kAtPowers = kWaves * 4 * kTileBytes, kBytes = kAtPowers + kWaves * 2 * kPowers;     // [wave][K0, V0, K1, V1], [wave][powers 0, 1]
 };
 
-// A wavefront's part of an item: its tiles w, w + 8, ... of the piece, its lane's row and what that has seen.
+__device__ __forceinline__ f32x4 mul32(bf16x8 v, bf16x8 p, f32x4 o) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o, 0, 0, 0); }
+
+// A wavefront's part of an item: its tiles w, w + kWaves, ... of the piece, its lane's row and what that has seen.
 struct FewPart {
   int w, n, n_full, t0, t1, pos;     // tiles; those that all rows see whole; the piece's first token, last one seen + 1; the row's position
   const bf16_t *q;                   // the row
@@ -50,9 +50,9 @@ template <int kD> struct FewState {
   }
 };
 
-template <int kD>
+template <int kD, int kWaves>
 __device__ __forceinline__ void few_of_bf16(const FewPart &x, const ServePages<bf16_t> &pages, float scale_log2, unsigned char *mine, FewState<kD> &st) {
-  constexpr int kWaves = kServeWaves, kTokens = 16, kRow = 2 * kD, kTileBytes = kTokens * kRow;
+  constexpr int kTokens = 16, kRow = 2 * kD, kTileBytes = kTokens * kRow;
   constexpr int kDB = kD / 16, kChunks = kRow / 16, kG = kRow / 64, kLoadRows = 64 / kChunks, kLoads = kTokens / kLoadRows;
   const int lane = threadIdx.x & 63, n16 = lane & 15, c4 = lane >> 4;
   // Row r's 16-byte chunk x is kept at x ^ swz(r): eight rows read at one chunk, or four groups of four rows read transposed, fall on
@@ -91,33 +91,31 @@ __device__ __forceinline__ void few_of_bf16(const FewPart &x, const ServePages<b
 #pragma unroll
     for (int g = 0; g < kG; ++g) {
       const u32x4 k = *reinterpret_cast<const u32x4 *>(K + n16 * kRow + (((4 * g + c4) ^ swz(n16)) << 4));
-      s[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[g]), s[0], 0, 0, 0);
+      s[0] = mul32(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[g]), s[0]);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more2) issue(pages.k, it + 2, 2 * buf);
     const int t = x.t0 + (x.w + it * kWaves) * kTokens;
-    float p[1][4], seen[4];
+    const auto sees = [&](int i) __attribute__((always_inline)) { return t + 4 * c4 + i <= min(x.pos, x.t1 - 1); };
     if constexpr (kMasked) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool vis = t + 4 * c4 + i <= min(x.pos, x.t1 - 1);
-        s[0][i] = vis ? s[0][i] : -INFINITY;
-        seen[i] = vis ? 1.f : 0.f;
-      }
+      for (int i = 0; i < 4; ++i) s[0][i] = sees(i) ? s[0][i] : -INFINITY;
     }
+    float p[1][4];
     st.softmax(s, p, scale_log2);
+    bf16x4 pb, ones;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      pb[i] = (__bf16)p[0][i];
+      if (kMasked) ones[i] = (__bf16)(sees(i) ? 1.f : 0.f);
+    }
     if (more2) wait_loads<3 * kLoads>();
     else if (more) wait_loads<2 * kLoads>();
     else wait_loads<0>();
     const int row = 4 * c4 + (n16 >> 2);
-    bf16x4 v[kDB], pb, ones;
+    bf16x4 v[kDB];
 #pragma unroll
     for (int db = 0; db < kDB; ++db) v[db] = lds_tr(V + row * kRow + (((2 * db + ((n16 >> 1) & 1)) ^ swz(row)) << 4) + 8 * (n16 & 1));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      pb[i] = (__bf16)p[0][i];
-      if (kMasked) ones[i] = (__bf16)seen[i];
-    }
     if constexpr (kMasked) {
       add_masked16(v, pb, ones, st.o);
     } else {
@@ -132,39 +130,28 @@ __device__ __forceinline__ void few_of_bf16(const FewPart &x, const ServePages<b
   for (; it < x.n; ++it) step(it, std::true_type());
 }
 
-__device__ __forceinline__ f32x4 mul32(bf16x8 v, bf16x8 p, f32x4 o) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o, 0, 0, 0); }
-// As add_masked16 (../paged/chunk_attn_16.hpp), of 32 keys.
-template <int kN> __device__ __forceinline__ void add_masked32(const bf16x8 (&v)[kN], bf16x8 p, bf16x8 seen, f32x4 *o) {
-  unsigned int any = 0u;
-#pragma unroll
-  for (int db = 0; db < kN; ++db)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) any |= not_finite(__builtin_bit_cast(u32x4, v[db])[i]);
-  if (__builtin_amdgcn_ballot_w64(any != 0u) == 0ull) {
-#pragma unroll
-    for (int db = 0; db < kN; ++db) o[db] = mul32(v[db], p, o[db]);
+// As add_masked16 (../paged/chunk_attn_16.hpp), of 32 keys and one block of columns.
+__device__ __forceinline__ void add_masked32(bf16x8 v, bf16x8 p, bf16x8 seen, f32x4 *o) {
+  u32x4 fine = __builtin_bit_cast(u32x4, v), up, down;
+  if (__builtin_amdgcn_ballot_w64((not_finite(fine[0]) | not_finite(fine[1]) | not_finite(fine[2]) | not_finite(fine[3])) != 0u) == 0ull) {
+    *o = mul32(v, p, *o);
     return;
   }
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int db = 0; db < kN; ++db) {
-    u32x4 fine = __builtin_bit_cast(u32x4, v[db]), up, down;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      up[i] = ones_of(fine[i], false);
-      down[i] = ones_of(fine[i], true);
-      fine[i] &= ~no_numbers(fine[i]);
-    }
-    o[db] = infinities(mul32(__builtin_bit_cast(bf16x8, fine), p, o[db]), mul32(__builtin_bit_cast(bf16x8, up), seen, zero),
-                       mul32(__builtin_bit_cast(bf16x8, down), seen, zero));
-    __builtin_amdgcn_sched_barrier(0);
+  for (int i = 0; i < 4; ++i) {
+    up[i] = ones_of(fine[i], false);
+    down[i] = ones_of(fine[i], true);
+    fine[i] &= ~no_numbers(fine[i]);
   }
+  *o = infinities(mul32(__builtin_bit_cast(bf16x8, fine), p, *o), mul32(__builtin_bit_cast(bf16x8, up), seen, zero),
+                  mul32(__builtin_bit_cast(bf16x8, down), seen, zero));
 }
 
-template <int kD>
+template <int kD, int kWaves>
 __device__ __forceinline__ void few_of_8bit(const FewPart &x, const ServePages<e4m3_t> &pages, float scale_log2, unsigned char *mine, unsigned char *powers,
                                             FewState<kD> &st) {
-  constexpr int kWaves = kServeWaves, kTokens = 32, kRow = kD, kTileBytes = kTokens * kRow, kPowers = FewTiles<e4m3_t, kD>::kPowers;
+  constexpr int kTokens = 32, kRow = kD, kTileBytes = kTokens * kRow, kPowers = FewTiles<e4m3_t, kD, kWaves>::kPowers;
   constexpr int kDB = kD / 16, kChunks = kRow / 16, kLoadRows = 64 / kChunks, kLoads = kTokens / kLoadRows, kReads = kChunks / 4;
   const int lane = threadIdx.x & 63, n16 = lane & 15, c4 = lane >> 4;
   // Row r's 16-byte chunk x is kept at x ^ swz(r): eight rows of K read at one chunk, or of V at one chunk transposed (four of either half of the tile),
@@ -229,17 +216,14 @@ __device__ __forceinline__ void few_of_8bit(const FewPart &x, const ServePages<e
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more2) issue_k(it + 2);
-    float p[2][4], seen[2][4];
+    const auto sees = [&](int k, int i) __attribute__((always_inline)) { return token_of(it) + 16 * k + 4 * c4 + i <= min(x.pos, x.t1 - 1); };
     if constexpr (kMasked) {
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bool vis = token_of(it) + 16 * k + 4 * c4 + i <= min(x.pos, x.t1 - 1);
-          s[k][i] = vis ? s[k][i] : -INFINITY;
-          seen[k][i] = vis ? 1.f : 0.f;
-        }
+        for (int i = 0; i < 4; ++i) s[k][i] = sees(k, i) ? s[k][i] : -INFINITY;
     }
+    float p[2][4];
     st.softmax(s, p, scale_log2);
     bf16x8 pb, ones;
 #pragma unroll
@@ -247,25 +231,22 @@ __device__ __forceinline__ void few_of_8bit(const FewPart &x, const ServePages<e
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         pb[4 * k + i] = (__bf16)(p[k][i] * power_in(pv[k][i >> 1], i, true));
-        if (kMasked) ones[4 * k + i] = (__bf16)seen[k][i];
+        if (kMasked) ones[4 * k + i] = (__bf16)(sees(k, i) ? 1.f : 0.f);
       }
     if (more2) wait_loads<3 * kLoads + 2>();
     else if (more) wait_loads<2 * kLoads + 1>();
     else wait_loads<0>();
     const int j = n16 >> 1, row = 4 * c4 + (j & 3) + 16 * (j >> 2);
-    bf16x8 v[kDB];
-#pragma unroll
-    for (int db = 0; db < kDB; ++db) {
+    const auto read_v = [&](int db) __attribute__((always_inline)) {
       typedef __attribute__((ext_vector_type(2))) int i32x2;
       const i32x2 codes = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(V + row * kRow + ((db ^ swz_v(row)) << 4) + 8 * (n16 & 1)));
       const u32x2 lo = four_of((unsigned int)codes[0], 1.f), hi = four_of((unsigned int)codes[1], 1.f);
-      v[db] = __builtin_bit_cast(bf16x8, (u32x4){lo[0], lo[1], hi[0], hi[1]});
-    }
-    if constexpr (kMasked) {
-      add_masked32(v, pb, ones, st.o);
-    } else {
+      return __builtin_bit_cast(bf16x8, (u32x4){lo[0], lo[1], hi[0], hi[1]});
+    };
 #pragma unroll
-      for (int db = 0; db < kDB; ++db) st.o[db] = mul32(v[db], pb, st.o[db]);
+    for (int db = 0; db < kDB; ++db) {
+      if constexpr (kMasked) add_masked32(read_v(db), pb, ones, &st.o[db]);
+      else st.o[db] = mul32(read_v(db), pb, st.o[db]);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more2) issue_v(it + 2);
@@ -275,10 +256,10 @@ __device__ __forceinline__ void few_of_8bit(const FewPart &x, const ServePages<e
   for (; it < x.n; ++it) step(it, std::true_type());
 }
 
-template <typename C, int kD>
+template <typename C, int kD, int kWaves>
 __device__ __forceinline__ void attend_few(const ServeArgs &a, const ServePiece &pc, int idx, int c, unsigned char *lds, float (*ml)[16][2]) {
-  using Tiles = FewTiles<C, kD>;
-  constexpr int kWaves = kServeWaves, kTokens = Tiles::kTokens, kDB = kD / 16, kOut = kD / 4;
+  using Tiles = FewTiles<C, kD, kWaves>;
+  constexpr int kTokens = Tiles::kTokens, kDB = kD / 16, kOut = kD / 4;
   const int lane = threadIdx.x & 63, n16 = lane & 15, c4 = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int R = pc.it.n * a.g;                             // (at most 16: one block)
@@ -302,8 +283,8 @@ __device__ __forceinline__ void attend_few(const ServeArgs &a, const ServePiece 
   if (x.n > 0) {
     const ServePages<C> pages = serve_pages<C>(a, pc.it, c);
     unsigned char *mine = lds + w * 4 * Tiles::kTileBytes;
-    if constexpr (Tiles::k8) few_of_8bit<kD>(x, pages, a.scale_log2, mine, lds + kWaves * 4 * Tiles::kTileBytes + w * 2 * Tiles::kPowers, st);
-    else few_of_bf16<kD>(x, pages, a.scale_log2, mine, st);
+    if constexpr (Tiles::k8) few_of_8bit<kD, kWaves>(x, pages, a.scale_log2, mine, lds + Tiles::kAtPowers + w * 2 * Tiles::kPowers, st);
+    else few_of_bf16<kD, kWaves>(x, pages, a.scale_log2, mine, st);
   }
   // ---- merge: states of the wavefronts through LDS
   __syncthreads();

@@ -49,9 +49,9 @@ struct ServeArgs {
   ServePiece *pieces;      // with groups: [slots], n_pieces of them
   int32_t *n_pieces;
 };
-// How a call of these sizes is run: rows per block, pieces per KV head at most, those that run at once, workgroups per KV head, floats of part_o and part_ml.
+// How a call of these sizes is run: rows per block, wavefronts per workgroup (16 rows), pieces per KV head at most, those that run at once, workgroups per KV head, floats of part_o and part_ml.
 struct ServeShape {
-  int rows, slots, round, grid;
+  int rows, waves, slots, round, grid;
   int64_t floats_o, floats_ml;
 };
 ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t n_rows, int max_new, int64_t capacity);
