@@ -62,6 +62,7 @@ template <typename T, int kD>
 __global__ void __launch_bounds__(256) mrope_append8_kernel(Append8Args a, Frequencies f) {
   constexpr int kHalf = kD / 2, kPer = Elem<T>::kPer16B, kParts = kHalf / kPer;
   __shared__ double cs[2][kHalf];
+  __shared__ float cs32[2][kHalf];
   const int n = blockIdx.x, tid = threadIdx.x;
   const int slot = a.slots[n];
   if ((unsigned)slot >= (unsigned)a.n_slots) return;      // uniform
@@ -69,6 +70,8 @@ __global__ void __launch_bounds__(256) mrope_append8_kernel(Append8Args a, Frequ
     const CosSin t = cos_sin(a.positions[f.axis[tid] * a.axis_stride + n], f.quarter[tid]);
     cs[0][tid] = t.c;
     cs[1][tid] = t.s;
+    cs32[0][tid] = (float)t.c;
+    cs32[1][tid] = (float)t.s;
   }
   __syncthreads();
   const int page = slot >> a.page_shift, token = slot & ((1 << a.page_shift) - 1);
@@ -87,7 +90,7 @@ __global__ void __launch_bounds__(256) mrope_append8_kernel(Append8Args a, Frequ
       T y0[kPer], y1[kPer];
 #pragma unroll
       for (int e = 0; e < kPer; ++e) {
-        const float co = (float)cs[0][i + e], si = (float)cs[1][i + e];
+        const float co = cs32[0][i + e], si = cs32[1][i + e];
         Elem<T>::store(&y0[e], x0[e] * co - x1[e] * si);
         Elem<T>::store(&y1[e], x1[e] * co + x0[e] * si);
       }
