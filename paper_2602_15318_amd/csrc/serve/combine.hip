@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) serve_combi
   const int n_blocks = serve_blocks(a, n);
   // (offsets that overlap: a plan that nobody has written)
   if (left.first < 0 || (int64_t)n_blocks * n_own > a.slots - left.first) return;
-  const int64_t group_rho = (int64_t)(r - left.group_row0) * a.g;
+  const int64_t group_rho = ((int64_t)r - left.group_row0) * a.g;
   if (n_shared > 0 && (left.group_first < 0 || left.group_blocks < 1 || (int64_t)left.group_blocks * n_shared > a.slots - left.group_first ||
                        group_rho < 0 || (group_rho + a.g - 1) >> a.block_shift >= left.group_blocks))
     return;
