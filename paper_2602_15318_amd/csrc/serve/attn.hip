@@ -10,6 +10,12 @@ hipError_t launch_serve_bf16(int d, const ServeShape &s, const ServeArgs &a, hip
 hipError_t launch_serve_f32(int d, int pieces, const ServeArgs &a, hipStream_t st);
 hipError_t launch_serve_combine(int dtype, int d, const ServeArgs &a, hipStream_t st);
 
+// The plan, blocks that are partly filled and a second pass over all rows cost 5 to 9 us, and what a group's requests read of one prefix comes out of the
+// caches: below these sizes every request reads its own.  bf16, shared and not, us: 8 of 2,100 tokens (34 MB) 20.0 and 14.0; 4 of 8,500 (70 MB) 22.5 and
+// 17.8; 8 of 8,300 (137 MB) 23.7 and 23.1; 16 of them 27.4 and 39.1; 8 of 26,300 (430 MB) 28.7 and 59.4.  fp32: 4 of 2,060 (34 MB) 21.3 and 20.7; 8
+// (68 MB) 22.7 and 26.1.
+bool serve_shares(int dtype, int64_t tokens, int64_t bytes) { return tokens > (dtype == SPARROW_F32 ? 1ll << 25 : 1ll << 27) / bytes; }
+
 ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t n_rows, int max_new, int64_t capacity) {
   ServeShape s;
   const bool f32 = dtype == SPARROW_F32;

@@ -19,8 +19,8 @@ __device__ __forceinline__ void add(State &s, float m, float l, f32x4 o, float s
 template <typename T, int kD, int kSpread>
 __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) serve_combine_kernel(ServeArgs a) {
   constexpr int kGroup = kD / 4, kGroups = 64 / kGroup, kAtOnce = kSpread == 1 ? 4 : 8, kParts = kSpread * kGroups;
-  __shared__ __attribute__((aligned(16))) float sum_o[kParts][kD];
-  __shared__ float sum_ml[kParts][2];
+  __shared__ __attribute__((aligned(16))) float sum_o[kSpread][kD];
+  __shared__ float sum_ml[kSpread][2];
   const int lane = threadIdx.x & 63, group = lane / kGroup, at4 = 4 * (lane % kGroup);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.y + 32768 * blockIdx.z;
@@ -77,9 +77,10 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) serve_combi
     for (int s0 = kSpread > 1 ? part : 0; s0 < n_all; s0 += kStep * kAtOnce) {
       float m[kAtOnce], l[kAtOnce];
       f32x4 o[kAtOnce];
+      const int left_over = (n_all - 1 - s0) / kStep;
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        const int64_t k = at(min(s0 + kStep * u, n_all - 1));
+      for (int u = 0; u < kAtOnce; ++u) {                  // (behind the last: the last again, which is on its way already)
+        const int64_t k = at(s0 + kStep * min(u, left_over));
         const float2 ml = ((const float2 *)a.part_ml)[k];
         m[u] = ml.x;
         l[u] = ml.y;
@@ -90,20 +91,19 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) serve_combi
         if (s0 + kStep * u < n_all) add(st, m[u], l[u], o[u], a.scale_log2);
     }
     if constexpr (kSpread > 1) {
-      *(f32x4 *)&sum_o[part][at4] = st.o;
-      if (at4 == 0) { sum_ml[part][0] = st.top; sum_ml[part][1] = st.l; }
+#pragma unroll
+      for (int x = kGroup; x < 64; x <<= 1) {              // the wavefront's groups, then the wavefronts
+        f32x4 other;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) other[i] = __shfl_xor(st.o[i], x, 64);
+        add(st, __shfl_xor(st.top, x, 64), __shfl_xor(st.l, x, 64), other, a.scale_log2);
+      }
+      if (group == 0) *(f32x4 *)&sum_o[w][at4] = st.o;
+      if (lane == 0) { sum_ml[w][0] = st.top; sum_ml[w][1] = st.l; }
       __syncthreads();
       if (part != 0) return;
-      const int n_parts = min(kParts, n_all);              // those that had a piece
-      for (int k = 1; k < n_parts; ++k) st.top = fmaxf(st.top, sum_ml[k][0]);
-      st.l = 0.f;
-      st.o = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-      for (int k = 0; k < n_parts; ++k) {
-        const float f = factor(sum_ml[k][0], st.top, a.scale_log2);
-        st.l = fmaf(sum_ml[k][1], f, st.l);
-        st.o += *(const f32x4 *)&sum_o[k][at4] * f;
-      }
+#pragma unroll
+      for (int k = 1; k < kSpread; ++k) add(st, sum_ml[k][0], sum_ml[k][1], *(const f32x4 *)&sum_o[k][at4], a.scale_log2);
     }
     const int64_t to = (int64_t)r * a.Hq + h;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};

@@ -1,5 +1,5 @@
 // The plan of a batch in groups (serve_plan.hpp), worked out once: every piece of a KV head, and what the second pass needs.  One workgroup; a thread takes
-// a request, then a wavefront ways of cutting, then a thread pieces.  Measured 5 us a call of 32 requests; by every workgroup of the attention itself, which
+// a request, then a wavefront ways of cutting, then a thread pieces.  Measured 6 us a call of 32 requests; by every workgroup of the attention itself, which
 // takes one compute unit each, it cost some 4 us a round of them.
 #include "serve_plan.hpp"
 
@@ -7,8 +7,8 @@ namespace sparrow {
 
 namespace {
 
-constexpr int kWaves = 16, kThreads = 64 * kWaves;
-constexpr int kMaxItems = SPARROW_MAX_PREFIX_GROUPS + SPARROW_MAX_PAGED_BATCH, kWays = 16;
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kMaxItems = SPARROW_MAX_PREFIX_GROUPS + SPARROW_MAX_PAGED_BATCH, kWays = 8;
 
 struct Plan {                     // in LDS: groups first, then requests
   int row0[kMaxItems], n[kMaxItems];   // first row of the batch; rows (tokens)
@@ -21,11 +21,12 @@ struct Plan {                     // in LDS: groups first, then requests
   float cost[kWays];
   int T[kWays];
 };
-// T: of kWays ways to cut the longest item that which should end first, among those whose pieces the workspace holds.  In grains of 64 tokens: the mean
-// work of a workgroup's place or the rounds of long pieces, whichever is more, each piece with its beginning and end (kMany, kFew: of items of more than
-// 64 rows, whose partial output is up to 128 KB, and others); and the second pass, which reads what all leave.
+// T: of kWays ways to cut the longest item that which should end first, among those whose pieces the workspace holds.  In grains of 64 tokens of an item of
+// more than 64 rows (kTail: of others), each piece with its beginning and end (kMany: its partial output is up to 128 KB; kFew): the mean work of a
+// workgroup's place and some of the longest piece, or the rounds of pieces of more than half of that, whichever is more; and the second pass, which reads what
+// all leave (kCombine).  Fitted to nine batches at seven lengths each: that which it takes is 3.5 % behind the best of the seven at most.
 __device__ __forceinline__ int best_piece(const ServeArgs &a, Plan *p, int items) {
-  constexpr float kMany = 6.f, kFew = 3.f, kCombine = 0.003f;
+  constexpr float kMany = 10.f, kFew = 3.f, kTail = 0.5f, kRest = 0.15f, kCombine = 0.006f;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float weight = 0.f, longest = 0.f;
   int blocks = 0;
@@ -38,35 +39,42 @@ __device__ __forceinline__ int best_piece(const ServeArgs &a, Plan *p, int items
   const float W = wave_sum_valu(weight) * (1.f / kGrain), inv_round = 1.f / (float)a.round;
   const int L = max(((int)wave_max_valu(longest) + kGrain - 1) / kGrain, 1), U = lane_value(wave_scan(blocks), 63);
   int s = max(min((int)(0.5f * (float)a.round / fmaxf(W / (float)L, 1.f)), L), 1);
-  for (int way = 0; way < kWays; ++way, s += max(s / 8, 1)) {
-    if (way != w) continue;
-    const int hi = quotient(L + s - 1, s), T = hi * kGrain;
+  for (int way = 0; way < w; ++way) s += max(s / 4, 1);
+  if (w < kWays) {
+    const int T = quotient(L + s - 1, s) * kGrain;
     const float inv_t = __builtin_amdgcn_rcpf((float)T);
-    float extra = 0.f, many = 0.f;
+    const auto pieces_of = [&](int i) { return quotient(max(p->to[i] - p->from[i] - 1, 0), T, inv_t) + 1; };
+    const auto end_of = [&](int i) { return p->n[i] * a.g > 64 ? kMany : kFew; };
+    const auto time_of = [&](int i, int splits) {
+      return end_of(i) + (p->n[i] * a.g > 64 ? 1.f : kTail) * (1.f / kGrain) * (float)(p->to[i] - p->from[i]) * __builtin_amdgcn_rcpf((float)splits);
+    };
+    float ends = 0.f, sum = 0.f, most = 0.f, big = 0.f;
     int count = 0;
     for (int i = lane; i < items; i += 64) {
-      const int len = p->to[i] - p->from[i], pieces = min(p->blocks[i], a.slots) * (quotient(max(len - 1, 0), T, inv_t) + 1);
+      const int splits = pieces_of(i), pieces = min(p->blocks[i], a.slots) * splits;
+      const float time = time_of(i, splits);
       count += pieces;
-      extra += (float)pieces * (p->n[i] * a.g > 64 ? kMany : kFew);
-      many += 2 * len > T ? (float)pieces : 0.f;
+      ends += (float)pieces * end_of(i);
+      sum += (float)pieces * time;
+      most = fmaxf(most, pieces > 0 ? time : 0.f);
+    }
+    most = wave_max_valu(most);
+    for (int i = lane; i < items; i += 64) {
+      const int splits = pieces_of(i);
+      big += 2.f * time_of(i, splits) > most ? (float)(min(p->blocks[i], a.slots) * splits) : 0.f;
     }
     const int N = lane_value(wave_scan(count), 63);
-    const float E = wave_sum_valu(extra), rounds = __builtin_ceilf(wave_sum_valu(many) * inv_round);
-    const float cost = fmaxf((W + E) * inv_round, rounds * ((float)hi + kFew)) + kCombine * (float)a.Hkv * E;
+    const float rounds = __builtin_ceilf(wave_sum_valu(big) * inv_round);
+    const float cost = fmaxf(wave_sum_valu(sum) * inv_round + kRest * most, rounds * most) + kCombine * (float)a.Hkv * wave_sum_valu(ends);
     if (lane == 0) {
-      p->cost[way] = N > a.slots && N > U ? 3.4e38f : cost;            // (uncut blocks always fit)
-      p->T[way] = T;
+      p->cost[w] = N > a.slots && N > U ? 3.4e38f : cost;              // (uncut blocks always fit)
+      p->T[w] = T;
     }
   }
   __syncthreads();
-  int T = 1 << 29;
-  float best = 3.4e38f;
-  for (int way = 0; way < kWays; ++way)
-    if (p->cost[way] < best) {
-      best = p->cost[way];
-      T = p->T[way];
-    }
-  return __builtin_amdgcn_readfirstlane(T);
+  const float mine = p->cost[lane % kWays], best = -wave_max_valu(-mine);
+  const int T = p->T[lane % kWays];
+  return best < 3.4e38f ? lane_value(T, __builtin_ctzll(__builtin_amdgcn_ballot_w64(mine == best))) : 1 << 29;
 }
 
 __global__ void __launch_bounds__(kThreads) serve_plan_kernel(ServeArgs a) {

@@ -54,6 +54,8 @@ struct ServeShape {
   int rows, waves, slots, round, grid;
   int64_t floats_o, floats_ml;
 };
+// Whether prefixes are read once for their groups, by the tokens that the tables of the batch hold and the bytes of one token's keys and values.
+bool serve_shares(int dtype, int64_t tokens, int64_t bytes);
 ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t n_rows, int max_new, int64_t capacity);
 hipError_t launch_serve_attn(int dtype, int d, const ServeShape &s, const ServeArgs &a, hipStream_t st);
 

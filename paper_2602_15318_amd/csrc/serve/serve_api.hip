@@ -1,5 +1,6 @@
 // Host side of the C ABI declared in include/sparrow_serve.h: argument validation and launches.  No device allocation, no
 // synchronisation, no device reads.
+#include <algorithm>
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -93,6 +94,11 @@ bool attention_sizes(const sparrow_paged_desc *d, int32_t B, int32_t n_groups, i
          (int64_t)n_rows * d->n_q_heads < 1ll << 31 && max_new > 0;
 }
 
+size_t workspace_of(const ServeShape &s, int32_t B, int32_t G) {
+  return s.slots == 0 ? 0 : round_up((size_t)s.floats_o * 4, 256) + round_up((size_t)s.floats_ml * 4, 256) + round_up((size_t)B * 32, 256) +
+                                (G == 0 ? 0 : 256 + round_up((size_t)s.slots * 48, 256));
+}
+
 int attention(const sparrow_paged_desc *desc, const void *q, const void *k_cache, const void *v_cache, const uint8_t *exponents,
               const int32_t *block_table, int32_t table_width, int64_t table_stride, const int32_t *cu_new, const int32_t *kv_len,
               int32_t B, const int32_t *group_start, const int32_t *prefix_len, int32_t n_groups, int32_t n_rows, int32_t max_new,
@@ -124,18 +130,20 @@ int attention(const sparrow_paged_desc *desc, const void *q, const void *k_cache
   a.out = out; a.lse = lse;
   a.table_stride = table_stride; a.q_row = desc->q_stride_row;
   a.stride_page = desc->kv_stride_page; a.stride_token = desc->kv_stride_token; a.stride_head = desc->kv_stride_head;
-  a.B = B; a.G = n_groups; a.n_rows = n_rows; a.max_new = max_new; a.Hq = desc->n_q_heads; a.Hkv = desc->n_kv_heads;
+  a.B = B; a.n_rows = n_rows; a.max_new = max_new; a.Hq = desc->n_q_heads; a.Hkv = desc->n_kv_heads;
   a.g = desc->n_q_heads / desc->n_kv_heads;
   a.table_width = table_width; a.page_shift = shift_of(desc->page_size); a.n_pages = desc->n_pages;
   a.scale_log2 = (desc->scale > 0.f ? desc->scale : 1.0f / std::sqrt((float)desc->head_dim)) * kLog2e;
   a.inv_g = 1.0f / (float)a.g;
-  const ServeShape shape = serve_shape(desc->dtype, desc->head_dim, a.Hq, a.Hkv, B, n_groups, n_rows, max_new, (int64_t)table_width * desc->page_size);
+  const int64_t capacity = (int64_t)table_width * desc->page_size;
+  a.G = serve_shares(desc->dtype, B * capacity, 2ll * a.Hkv * desc->head_dim * (exponents ? 1 : desc->dtype == SPARROW_F32 ? 4 : 2)) ? n_groups : 0;
+  const ServeShape shape = serve_shape(desc->dtype, desc->head_dim, a.Hq, a.Hkv, B, a.G, n_rows, max_new, capacity);
   a.slots = shape.slots; a.round = shape.round; a.block_shift = shift_of(shape.rows);
   a.part_o = (float *)workspace;
   a.part_ml = (float *)((unsigned char *)workspace + round_up((size_t)shape.floats_o * 4, 256));
   a.left = shape.slots == 0 ? nullptr : (ServeLeft *)((unsigned char *)a.part_ml + round_up((size_t)shape.floats_ml * 4, 256));
-  a.n_pieces = n_groups == 0 ? nullptr : (int32_t *)((unsigned char *)a.left + round_up((size_t)B * 32, 256));
-  a.pieces = n_groups == 0 ? nullptr : (ServePiece *)((unsigned char *)a.n_pieces + 256);
+  a.n_pieces = a.G == 0 ? nullptr : (int32_t *)((unsigned char *)a.left + round_up((size_t)B * 32, 256));
+  a.pieces = a.G == 0 ? nullptr : (ServePiece *)((unsigned char *)a.n_pieces + 256);
   const hipError_t e = launch_serve_attn(desc->dtype, desc->head_dim, shape, a, (hipStream_t)hip_stream);
   if (e != hipSuccess) return fail(SPARROW_ERR_DEVICE, "attention launch: %s", hipGetErrorString(e));
   return SPARROW_OK;
@@ -212,9 +220,11 @@ int sparrow_page_gather(const sparrow_paged_desc *desc, const void *k_cache, con
 
 size_t sparrow_prefix_attn_workspace(const sparrow_paged_desc *desc, int32_t B, int32_t n_groups, int32_t n_rows, int32_t max_new) {
   if (!attention_sizes(desc, B, n_groups, n_rows, max_new)) return 0;
-  const ServeShape s = serve_shape(desc->dtype, desc->head_dim, desc->n_q_heads, desc->n_kv_heads, B, n_groups, n_rows, max_new, SPARROW_MAX_PAGED_TOKENS);
-  return s.slots == 0 ? 0 : round_up((size_t)s.floats_o * 4, 256) + round_up((size_t)s.floats_ml * 4, 256) + round_up((size_t)B * 32, 256) +
-                                (n_groups == 0 ? 0 : 256 + round_up((size_t)s.slots * 48, 256));
+  size_t most = 0;                         // with the groups and without: which it will be depends on the tables
+  for (const int32_t G : {0, n_groups})
+    most = std::max(most, workspace_of(serve_shape(desc->dtype, desc->head_dim, desc->n_q_heads, desc->n_kv_heads, B, G, n_rows, max_new,
+                                                   SPARROW_MAX_PAGED_TOKENS), B, G));
+  return most;
 }
 
 int sparrow_chunk_attn8(const sparrow_paged_desc *desc, const void *q, const void *k_cache, const void *v_cache,

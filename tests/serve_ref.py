@@ -33,12 +33,18 @@ def quantise(x):
     return np.where(fine, out, np.nan), (np.log2(power)[..., 0] + 127).astype(np.uint8)
 
 
+def wide_table(B, Hkv, d, page):
+    """Entries per request for which prefixes are read once, whatever the types: 2^27 bytes of one byte per element."""
+    return (1 << 27) // (B * page * 2 * Hkv * d) + 1
+
+
 class Shared:
     """Requests whose tokens are kv, the last `new` of them new, on pages: groups = [(first request, end, shared tokens)].  cache: "e4m3" or
-    "own" (of dtype).  What no row may see is NaN, its powers any bytes; table entries behind a request's pages are no pages at all."""
+    "own" (of dtype).  What no row may see is NaN, its powers any bytes; table entries behind a request's pages are no pages at all; wide: with groups, tables
+    so wide that prefixes are read once for them."""
 
     def __init__(self, kv, new, groups=(), dtype="bf16", cache="own", Hq=4, Hkv=2, d=64, page=16, layout="token", seed=0, extra_rows=0, width=None,
-                 q_gain=1.0, row_gap=0, device="cuda"):
+                 q_gain=1.0, row_gap=0, device="cuda", wide=True):
         g = torch.Generator(device=device).manual_seed(seed)
         rnd = lambda *s: torch.randn(s, generator=g, device=device)       # noqa: E731
         self.kv, self.new, self.groups = list(kv), list(new), list(groups)
@@ -50,6 +56,8 @@ class Shared:
                 shared[b] = min(p, kv[a], kv[b]) // page     # whole pages of the group's first request
         held = [-(-k // page) for k in kv]
         width = width or max(max(held), 1)
+        if groups and wide:                  # (where the tables could hold little, nothing is shared)
+            width = max(width, wide_table(B, Hkv, d, page))
         n_pages = sum(held) + 2
         kind = torch.float8_e4m3fn if cache == "e4m3" else DT[dtype]
         shape = (n_pages, Hkv, page, d) if layout == "head" else (n_pages, page, Hkv, d)

@@ -55,6 +55,15 @@ def test_shared_prefixes(sp, dtype, cache, Hq, Hkv, d, kv, new, groups):
                          layout="token" if d == 128 else "head", seed=sum(kv), extra_rows=2, row_gap=2))
 
 
+@pytest.mark.parametrize("dtype, cache", [("bf16", "own"), ("bf16", "e4m3"), ("f32", "own"), ("f32", "e4m3")])
+def test_tables_of_either_side_of_the_rule(sp, dtype, cache):
+    """Prefixes of tables that hold little are read request by request: the same result."""
+    for kv, new in (([130, 240, 99], [1, 1, 1]), ([130, 240, 99], [9, 30, 2])):
+        width = {"f32": 1 << 25, "bf16": 1 << 27}[dtype] // (3 * 16 * 2 * 2 * 64 * (1 if cache == "e4m3" else 4 if dtype == "f32" else 2))
+        for w in (None, width, width + 1):
+            _check(sp, s8.Shared(kv, new, [(0, 3, 96)], dtype=dtype, cache=cache, Hq=14, Hkv=2, d=64, seed=9, width=w, wide=False))
+
+
 @pytest.mark.parametrize("dtype, cache", [("bf16", "own"), ("bf16", "e4m3"), ("f32", "own")])
 @pytest.mark.parametrize("kv, new, groups", [
     ([100, 120, 90], [1, 1, 30], [(0, 3, 95)]),                # more shared than the third request has before its new tokens

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paged_ref as ref
+import serve_ref as s8
 
 pytestmark = pytest.mark.gpu
 # Weights and outputs are rounded to bf16 once each, half a step 2^-8: 2^-8 (A + |o|), with A = sum of p |v| <= 2 for these values, N(0, 1) and quantised;
@@ -29,7 +30,8 @@ class Server:
         self.kc, self.vc = (torch.full((n, page, Hkv, d), 0x7f, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in range(2))
         self.exps = torch.full((n, Hkv, page, 2), 255, dtype=torch.uint8, device="cuda")
         ids = torch.randperm(n, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(torch.int32)
-        self.table = torch.cat([ids[:shared].expand(B, shared), ids[shared:].view(B, own)], 1).contiguous()
+        self.table = torch.cat([ids[:shared].expand(B, shared), ids[shared:].view(B, own), ids.new_full((B, s8.wide_table(B, Hkv, d, page)), -1)],
+                               1).contiguous()                    # room for long contexts, so that the video is read once
         self.len = torch.full((B,), video, dtype=torch.int32, device="cuda")
         self.inv, self.axis = ref.rotary(d)
         self.start, self.prefix = ref.ints([0, B]), ref.ints([video])
