@@ -75,6 +75,12 @@ def test_batches_of_every_size(sp, cache):
             _check(sp, s8.Shared(kv, [1] * B, cache=cache, Hq=2 * Hkv, Hkv=Hkv, d=64, seed=B, width=width), groups=cache == "own")
 
 
+@pytest.mark.parametrize("cache", ["own", "e4m3"])
+def test_batches_of_heads_of_128(sp, cache):
+    for B in (13, 48):
+        _check(sp, s8.Shared([1 + (41 * b) % 600 for b in range(B)], [1] * B, cache=cache, Hq=8, Hkv=4, d=128, seed=B, width=40), groups=cache == "own")
+
+
 def test_a_workspace_for_calls_one_after_the_other(sp):
     """What an earlier call has left there does not matter."""
     ws = torch.full((1 << 28,), 0xff, dtype=torch.uint8, device="cuda")
