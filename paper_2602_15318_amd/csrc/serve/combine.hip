@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) serve_combi
     return;
   const bool none = past + i < 0;
   const int part = w * kGroups + group;                    // kSpread 1: the head; else which of the pieces
-  for (int h = kSpread > 1 ? (int)blockIdx.x : part; h < a.Hq; h += kSpread > 1 ? a.Hq : 4 * kGroups) {
+  for (int h = kSpread > 1 ? (int)blockIdx.x : 4 * kGroups * blockIdx.x + part; h < a.Hq; h += kSpread > 1 ? a.Hq : 4 * kGroups * gridDim.x) {
     const int c = quotient(h, a.g, a.inv_g), of_group = h - c * a.g;
     const auto row_of = [&](int first, int blocks, int rho) {
       return (((int64_t)(first + blocks - 1 - (rho >> a.block_shift)) * a.Hkv + c) << a.block_shift) + (rho & ((1 << a.block_shift) - 1));
@@ -120,9 +120,9 @@ template <typename T, int kD> hipError_t launch(const ServeArgs &a, hipStream_t 
   const int y = a.n_rows < 32768 ? a.n_rows : 32768, z = (a.n_rows + 32767) / 32768;
   // as many wavefronts a (row, head) as the chip holds
   const int64_t rows = (int64_t)a.n_rows * a.Hq;
-  if (rows <= 1024) hipLaunchKernelGGL((serve_combine_kernel<T, kD, 8>), dim3(a.Hq, y, z), dim3(512), 0, st, a);
-  else if (rows <= 4096) hipLaunchKernelGGL((serve_combine_kernel<T, kD, 2>), dim3(a.Hq, y, z), dim3(128), 0, st, a);
-  else hipLaunchKernelGGL((serve_combine_kernel<T, kD, 1>), dim3(1, y, z), dim3(256), 0, st, a);
+  if (rows <= 256) hipLaunchKernelGGL((serve_combine_kernel<T, kD, 8>), dim3(a.Hq, y, z), dim3(512), 0, st, a);
+  else if (rows <= 3200) hipLaunchKernelGGL((serve_combine_kernel<T, kD, 2>), dim3(a.Hq, y, z), dim3(128), 0, st, a);
+  else hipLaunchKernelGGL((serve_combine_kernel<T, kD, 1>), dim3((a.Hq + 1024 / kD - 1) / (1024 / kD), y, z), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
