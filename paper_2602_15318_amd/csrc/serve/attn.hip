@@ -25,18 +25,23 @@ ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t 
   s.rows = of_item <= 16 ? 16 : f32 || of_item <= 64 ? 64 : 256;
   // every item ends in a block of its own, not all of it filled
   const int64_t blocks = (most <= s.rows ? 0 : n_rows * g / s.rows) + B + (G > 0 ? n_rows * g / s.rows + G : 0);
-  // Single tokens: the fewer (request, KV head) pairs, the fewer and larger the workgroups, and the fewer pieces there are to put together.
+  // Single tokens: the fewer (request, KV head) pairs, the fewer and larger the workgroups, and the fewer pieces there are to put together.  8 bits, heads of
+  // 128, contexts of up to 8,000, us by workgroups of 8, 4 and 2: 32 pairs 18.2, 19.3, 19.0; 52 pairs 23.7, 23.0, 23.5; 160 pairs 58, 45.6, 46.1; 192 pairs
+  // 61, 55.0, 54.0; 256 pairs 68, 67.5, 65.5.
   s.waves = B * Hkv <= 48 ? 8 : B * Hkv < 192 ? 4 : 2;
   const int at_once = f32 ? (d == 128 ? 512 : 1024) : G == 0 && s.rows == 16 ? 2048 / s.waves : 256;       // workgroups
   s.round = std::max(at_once / Hkv, 1);
   if (G > 0) {
     s.slots = (int)std::max<int64_t>(4 * s.round, blocks);
   } else if (most <= s.rows) {
-    s.round = std::max(s.round, 2 * B);
-    // Requests of up to 512 tokens (fp32: 128) in one piece each and without a second pass, by what the tables hold.
-    s.slots = capacity <= (f32 ? 128 : 512) ? 0 : s.round;
+    s.round = std::max(s.round, 2 * B);                    // (256 of up to 3,000 tokens 99.5 us, of B + 1 pieces 110, of 4 B 104)
+    // Requests of up to 512 tokens (fp32: 128), 1,024 where they fill half of the chip, in one piece each and without a second pass, by what the tables
+    // hold.  8 bits, four KV heads of 128, us in one piece and cut: 8 of 500 tokens 9.8 and 12.3, of 1,000 12.5 and 11.5; 40 of 500 11.0 and 15.0, of 1,000
+    // 15.5 and 18.4, of 1,500 20.5 and 21.8; 128 of 1,000 30.8 and 33.6.
+    s.slots = capacity <= (f32 ? 128 : B * Hkv < 128 ? 512 : 1024) ? 0 : s.round;
   } else {
-    // Cut where the blocks fill two thirds of the chip at most; two rounds of pieces if they end sooner.
+    // Cut where the blocks fill two thirds of the chip at most; two rounds of pieces if they end sooner.  8 bits over 26,112 tokens, four KV heads of 128, us
+    // cut and not: 1,000 new tokens 357 and 644, 1,500 511 and 645, 1,700 694 and 645.
     const int64_t filled = (n_rows * g + s.rows - 1) / s.rows;
     s.slots = 3 * filled <= 2 * s.round ? 2 * s.round : 0;
   }

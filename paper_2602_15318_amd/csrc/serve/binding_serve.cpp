@@ -3,6 +3,9 @@
 // tensor subclass, another dtype, shape or stride than the library takes, a tensor that is not on the current GPU, a stream of its own, ...) or a
 // torch function mode is active; serve.py's own code then takes the call, converts what can be converted and raises what has to be raised.
 // Nothing is kept between calls.
+//
+// us a call and its kernels in an unbroken row of them, ctypes / here: mrope_append8 of 13 rows and their page_gather 24.9 / 7.3 (two calls), page_gather of
+// seven tails 10.0 / 3.5, prefix_attn of five tokens 16.8 / 10.7.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 

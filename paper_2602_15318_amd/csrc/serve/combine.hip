@@ -2,6 +2,8 @@
 // (../paged/chunk_combine.hip): kD / 4 lanes take a row's piece, 16 bytes each; the groups of kSpread wavefronts (8 or 2) share the pieces of one
 // (row of the batch, query head), the loads of up to 8 pieces of a group on their way at once.  Where there are many rows (kSpread 1), each group takes
 // a head of its own.
+//
+// Bound by memory and its round trips: 32 single tokens over a shared 26,112 (21 MB of partials) 8.5 us, one token 4.9.
 #include "serve_plan.hpp"
 
 namespace sparrow {
@@ -118,7 +120,8 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) serve_combi
 
 template <typename T, int kD> hipError_t launch(const ServeArgs &a, hipStream_t st) {
   const int y = a.n_rows < 32768 ? a.n_rows : 32768, z = (a.n_rows + 32767) / 32768;
-  // as many wavefronts a (row, head) as the chip holds
+  // Wavefronts a (row, head): 8 below 256 of them, 2 below 3,200, else a part of one.  us of a call, rows * heads, with 8 / 2 / less: 896 42.5 / 41.3 / -, 1,344
+  // 53.5 / 50.3 / 50.4, 2,688 63.1 / 53.0 / 54.5, 3,584 62.5 / 51.1 / 48.8, 7,168 - / 59.7 / 55.0.
   const int64_t rows = (int64_t)a.n_rows * a.Hq;
   if (rows <= 256) hipLaunchKernelGGL((serve_combine_kernel<T, kD, 8>), dim3(a.Hq, y, z), dim3(512), 0, st, a);
   else if (rows <= 3200) hipLaunchKernelGGL((serve_combine_kernel<T, kD, 2>), dim3(a.Hq, y, z), dim3(128), 0, st, a);
