@@ -41,9 +41,10 @@ ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t 
     s.slots = capacity <= (f32 ? 128 : B * Hkv < 128 ? 512 : 1024) ? 0 : s.round;
   } else {
     // Cut where the blocks fill two thirds of the chip at most; two rounds of pieces if they end sooner.  8 bits over 26,112 tokens, four KV heads of 128, us
-    // cut and not: 1,000 new tokens 357 and 644, 1,500 511 and 645, 1,700 694 and 645.
+    // cut and not: 1,000 new tokens 357 and 644, 1,500 511 and 645, 1,700 694 and 645.  Nothing is cut off two tiles: 100 over 100 21.7 and 19.3, with heads
+    // of 64 18.3 and 11.4; 75 over 300 23.3 and 23.9, 17.9 and 18.9.
     const int64_t filled = (n_rows * g + s.rows - 1) / s.rows;
-    s.slots = 3 * filled <= 2 * s.round ? 2 * s.round : 0;
+    s.slots = capacity > 128 && 3 * filled <= 2 * s.round ? 2 * s.round : 0;
   }
   s.grid = (int)std::max<int64_t>(s.slots, G > 0 ? 0 : blocks);
   const int64_t units = (int64_t)s.slots * Hkv * s.rows;

@@ -15,11 +15,12 @@ __global__ void __launch_bounds__(64 * kWaves, 2) serve_attn_kernel(ServeArgs a)
   constexpr int kFew = FewTiles<C, kD, kWaves>::kBytes, kMany = ManyTiles<kD>::kBytes, kBytes = kFew > kMany ? kFew : kMany;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kBytes];
   __shared__ float ml[kWaves][16][2];
+  __shared__ int flags[kWaves];
   const int c = blockIdx.x, idx = blockIdx.y + 32768 * blockIdx.z;
   ServePiece pc;
   if (!serve_piece(a, idx, &pc)) return;              // uniform
   if (pc.it.n * a.g <= 16) attend_few<C, kD, kWaves>(a, pc, idx, c, lds, ml);
-  else attend_many<C, kD>(a, pc, idx, c, lds);
+  else attend_many<C, kD>(a, pc, idx, c, lds, flags);
 }
 
 // Calls without groups whose requests have 16 rows at most

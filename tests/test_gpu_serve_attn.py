@@ -104,6 +104,19 @@ def test_values_that_are_no_numbers_stay_where_they_are_seen(sp):
             _check(sp, x)
 
 
+@pytest.mark.parametrize("cache", ["own", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kv, new", [([720], [100]), ([128, 320], [128, 40]), ([96], [90]), ([64], [64]), ([1600, 160], [300, 33])])
+def test_tiles_that_some_rows_do_not_see_whole(sp, cache, d, kv, new):
+    """Contexts that fill their pages, so that nothing around them is a NaN; then one of a later row's values is, and one of an earlier row's."""
+    x = s8.Shared(kv, new, cache=cache, Hq=14, Hkv=2, d=d, seed=11)
+    _check(sp, x)
+    bads = [float("nan")] if cache == "e4m3" else [float("inf"), float("nan")]
+    for bad, t in zip(bads * 3, (kv[0] - 1, kv[0] - new[0] // 2, max(kv[0] - new[0] - 1, 0))):
+        x.put(0, t, V=bad)
+        _check(sp, x)
+
+
 def test_exponents_of_any_byte(sp):
     x = s8.Shared([300, 310], [3, 40], [(0, 2, 200)], cache="e4m3", Hq=8, Hkv=2, d=128, seed=5)
     for b in range(2):
