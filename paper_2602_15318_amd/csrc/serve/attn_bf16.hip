@@ -1,8 +1,8 @@
 // Attention of new tokens in bf16 over a paged cache of bf16 or of 8 bits, prefixes of groups first: a workgroup of eight wavefronts takes a
 // piece of an item, of up to 16 rows (attn_few.hpp, bound by memory) or more (attn_many.hpp, bound by the matrix cores and, beside them, by the
 // exponentials).  In one launch, so that prefixes run beside what is behind them.
-#include "attn_few.hpp"
 #include "attn_many.hpp"
+#include "attn_some.hpp"
 
 namespace sparrow {
 
@@ -34,9 +34,26 @@ __global__ void __launch_bounds__(64 * kW, 2) serve_few_kernel(ServeArgs a) {
   attend_few<C, kD, kW>(a, pc, idx, c, lds, ml);
 }
 
+// Calls without groups over an 8-bit cache whose requests have 64 rows at most.  (A kernel of its own: in the one above it has too few scalar registers.)
+template <int kD>
+__global__ void __launch_bounds__(64 * kWaves, 2) serve_some_kernel(ServeArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[FewTiles<e4m3_t, kD, kWaves>::kBytes];
+  __shared__ float ml[kWaves][32][2];
+  const int c = blockIdx.x, idx = blockIdx.y + 32768 * blockIdx.z;
+  ServePiece pc;
+  if (!serve_find_piece(a, idx, &pc)) return;         // uniform
+  if (pc.it.n * a.g <= 16) attend_few<e4m3_t, kD, kWaves>(a, pc, idx, c, lds, (float (*)[16][2])ml);
+  else attend_some<kD>(a, pc, idx, c, lds, ml);
+}
+
 template <typename C, int kD> hipError_t launch(const ServeShape &s, const ServeArgs &a, hipStream_t st) {
   const dim3 grid(a.Hkv, s.grid < 32768 ? s.grid : 32768, (s.grid + 32767) / 32768);
   const auto run = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, st, a); };
+  if constexpr (std::is_same<C, e4m3_t>::value)
+    if (a.G == 0 && s.rows == 64) {
+      run(serve_some_kernel<kD>, kWaves);
+      return hipGetLastError();
+    }
   if (a.G > 0 || s.rows > 16) run(serve_attn_kernel<C, kD>, kWaves);
   else if (s.waves == 8) run(serve_few_kernel<C, kD, 8>, 8);
   else if (s.waves == 4) run(serve_few_kernel<C, kD, 4>, 4);

@@ -117,6 +117,21 @@ def test_tiles_that_some_rows_do_not_see_whole(sp, cache, d, kv, new):
         _check(sp, x)
 
 
+@pytest.mark.parametrize("Hq, Hkv, d", [(28, 4, 128), (8, 8, 64), (8, 1, 128), (14, 2, 64)])
+@pytest.mark.parametrize("kv, new", [([1900, 700, 64], [3, 4, 1]), ([900], [8]), ([33, 17, 8, 0, 2], [8, 1, 8, 0, 2]), ([512, 96, 31], [8, 8, 8])])
+def test_chains_over_8_bits(sp, Hq, Hkv, d, kv, new):
+    """17 to 64 rows a request and fewer; one new token's value a NaN at the end."""
+    for more in (1, 4) if Hq == Hkv else (1,):             # (one query head a group: 4 to 32 tokens)
+        n = [min(more * x, k) for x, k in zip(new, kv)]
+        x = s8.Shared(kv, n, cache="e4m3", Hq=Hq, Hkv=Hkv, d=d, page=16, seed=sum(kv), extra_rows=1)
+        _check(sp, x, groups=False)
+        x.put(0, kv[0] - 2, V=float("nan"))
+        _check(sp, x, groups=False)
+    for rows in (17, 32, 33, 64):
+        if Hq // Hkv == 1:
+            _check(sp, s8.Shared([rows + 80, rows], [rows, rows], cache="e4m3", Hq=Hq, Hkv=Hkv, d=d, seed=rows, width=80), groups=False)
+
+
 def test_exponents_of_any_byte(sp):
     x = s8.Shared([300, 310], [3, 40], [(0, 2, 200)], cache="e4m3", Hq=8, Hkv=2, d=128, seed=5)
     for b in range(2):
