@@ -65,7 +65,7 @@ int sparrow_chunk_attn8(const sparrow_paged_desc *desc, const void *q, const voi
  * sparrow_chunk_attn for requests that share prefixes: requests group_start[g] .. group_start[g+1]-1 of the batch begin with the same
  * prefix_len[g] tokens, and each group's prefix is read once for the new tokens of all its requests.  out and lse are what
  * sparrow_chunk_attn gives for the same tables.
- * Where the tables of the batch hold little (B * table_width * page_size tokens of 128 MB of K and V of all heads at most, 32 MB for fp32), a plan
+ * Where the tables of the batch hold little (B * table_width * page_size tokens of 200 MiB of K and V of all heads at most, 32 MiB for fp32), a plan
  * for groups costs more than it saves, and every request reads its own: n_groups changes nothing then.
  *
  *  exponents    dev uint8 of an 8-bit cache; NULL: the cache is of desc->dtype

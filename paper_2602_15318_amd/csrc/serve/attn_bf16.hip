@@ -34,27 +34,23 @@ __global__ void __launch_bounds__(64 * kW, 2) serve_few_kernel(ServeArgs a) {
   attend_few<C, kD, kW>(a, pc, idx, c, lds, ml);
 }
 
-// Calls without groups over an 8-bit cache whose requests have 64 rows at most.  (A kernel of its own: in the one above it has too few scalar registers.)
-template <int kD>
+// Calls without groups whose requests have 64 rows at most.  (A kernel of its own: in the one above it has too few scalar registers.)
+template <typename C, int kD>
 __global__ void __launch_bounds__(64 * kWaves, 2) serve_some_kernel(ServeArgs a) {
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[FewTiles<e4m3_t, kD, kWaves>::kBytes];
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[FewTiles<C, kD, kWaves>::kBytes];
   __shared__ float ml[kWaves][32][2];
   const int c = blockIdx.x, idx = blockIdx.y + 32768 * blockIdx.z;
   ServePiece pc;
   if (!serve_find_piece(a, idx, &pc)) return;         // uniform
-  if (pc.it.n * a.g <= 16) attend_few<e4m3_t, kD, kWaves>(a, pc, idx, c, lds, (float (*)[16][2])ml);
-  else attend_some<kD>(a, pc, idx, c, lds, ml);
+  if (pc.it.n * a.g <= 16) attend_few<C, kD, kWaves>(a, pc, idx, c, lds, (float (*)[16][2])ml);
+  else attend_some<C, kD>(a, pc, idx, c, lds, ml);
 }
 
 template <typename C, int kD> hipError_t launch(const ServeShape &s, const ServeArgs &a, hipStream_t st) {
   const dim3 grid(a.Hkv, s.grid < 32768 ? s.grid : 32768, (s.grid + 32767) / 32768);
   const auto run = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, st, a); };
-  if constexpr (std::is_same<C, e4m3_t>::value)
-    if (a.G == 0 && s.rows == 64) {
-      run(serve_some_kernel<kD>, kWaves);
-      return hipGetLastError();
-    }
-  if (a.G > 0 || s.rows > 16) run(serve_attn_kernel<C, kD>, kWaves);
+  if (a.G == 0 && s.rows == 64) run(serve_some_kernel<C, kD>, kWaves);
+  else if (a.G > 0 || s.rows > 16) run(serve_attn_kernel<C, kD>, kWaves);
   else if (s.waves == 8) run(serve_few_kernel<C, kD, 8>, 8);
   else if (s.waves == 4) run(serve_few_kernel<C, kD, 4>, 4);
   else run(serve_few_kernel<C, kD, 2>, 2);

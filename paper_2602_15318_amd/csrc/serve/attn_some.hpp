@@ -1,22 +1,24 @@
-// Attention of 17 to 64 rows (new token, query head of the group) of an item over an 8-bit cache, by eight wavefronts: chains of draft tokens, a prefix that a
-// few requests share.  As attn_few.hpp, with products of 32 rows: a wavefront has up to 32 rows and every eighth tile of 32 keys, or, of more rows, half of the
+// Attention of 17 to 64 rows (new token, query head of the group) of a request by eight wavefronts: chains of draft tokens.  As attn_few.hpp, with products of 32 rows: a wavefront has up to 32 rows and every eighth tile of 32 keys, or, of more rows, half of the
 // rows and every fourth tile; the states of a row are merged at the end.
 //
-// S^T = K Q^T by 32x32x16 products, P^T the scores' own registers (../paged/chunk_attn_mfma.hpp).  Codes lie in LDS as they come; they become bf16 numbers in
-// the operands, K's times its power, V's as they are, V's power in the probability.  A 16-byte read of K is a lane's part of two k-steps, Q^T cut alike; V^T of
+// S^T = K Q^T by 32x32x16 products, P^T the scores' own registers (../paged/chunk_attn_mfma.hpp).  Tiles go memory -> LDS past the registers.  A bf16 cache's
+// have one place of K and one of V a wavefront: K of the next is asked for behind the scores, V behind the output, and the other wavefronts
+// fill the time.  An 8-bit cache's have two, and their codes lie in LDS as they come; they become bf16 numbers in the operands, K's times its power, V's as they are, V's power in the probability.  A 16-byte read of K is a lane's part of two k-steps, Q^T cut alike; V^T of
 // eight keys is one transposing read of bytes (attn_few.hpp).
 //
 // Bound by memory and the round trips around it: twelve chains of 8 over up to 8,000, 28 and 4 heads of 128, 34.7 us with the second pass (in blocks of 256 rows
-// 44.4), one over 26,112 21.4 (24.7), with heads of 64 eight chains 27.0 (36.4).
+// 44.4), one over 26,112 21.4 (24.7), with heads of 64 eight chains 27.0 (36.4), all 8 bits; in bf16 twelve chains over 8,300 35.0 (44.4).
 #pragma once
 #include "attn_few.hpp"
 
 namespace sparrow {
 
-template <int kD>
+template <typename C, int kD>
 __device__ __forceinline__ void attend_some(const ServeArgs &a, const ServePiece &pc, int idx, int c, unsigned char *lds, float (*ml)[32][2]) {
-  constexpr int kWaves = 8, kTokens = 32, kRow = kD, kTileBytes = kTokens * kRow, kPowers = FewTiles<e4m3_t, kD, kWaves>::kPowers;
-  constexpr int kDB = kD / 32, kChunks = kRow / 16, kLoadRows = 64 / kChunks, kLoads = kTokens / kLoadRows, kReads = kChunks / 2, kOut = kD / 4;
+  constexpr bool k8 = std::is_same<C, e4m3_t>::value;
+  constexpr int kWaves = 8, kTokens = 32, kRow = kD * (int)sizeof(C), kTileBytes = kTokens * kRow, kPlace = 4 * kTokens * kD;
+  constexpr int kPowers = FewTiles<e4m3_t, kD, kWaves>::kPowers, kDB = kD / 32, kChunks = kRow / 16, kLoadRows = 64 / kChunks, kLoads = kTokens / kLoadRows;
+  constexpr int kReads = kD / 32, kOut = kD / 4;
   const int lane = threadIdx.x & 63, n32 = lane & 31, h = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int R = pc.it.n * a.g, shift = R > 32 ? 1 : 0, half = w & shift, stream = w >> shift, streams = kWaves >> shift;
@@ -24,17 +26,17 @@ __device__ __forceinline__ void attend_some(const ServeArgs &a, const ServePiece
   const int t1 = min(pc.t1, min(pc.it.past + pc.it.n, pc.it.to)), last_seen = min(min(pc.it.past + i_row, pc.it.to - 1), t1 - 1);
   const auto mine_of = [&](int tiles) { return max(tiles - stream + streams - 1, 0) >> (3 - shift); };
   const int n = mine_of(max(t1 - pc.t0 + kTokens - 1, 0) / kTokens), n_full = mine_of(max(min(pc.it.past + 1, t1) - pc.t0, 0) / kTokens);
-  unsigned char *const mine = lds + w * 4 * kTileBytes, *const powers = lds + kWaves * 4 * kTileBytes + w * 2 * kPowers;
+  unsigned char *const mine = lds + w * kPlace, *const powers = lds + kWaves * kPlace + w * 2 * kPowers;
   f32x16 o[kDB];
   float m = kNothingSeen, l = 0.f;
 #pragma unroll
   for (int db = 0; db < kDB; ++db) o[db] = (f32x16){0.f};
   if (n > 0) {
-    const ServePages<e4m3_t> pages = serve_pages<e4m3_t>(a, pc.it, c);
+    const ServePages<C> pages = serve_pages<C>(a, pc.it, c);
     // Row r's 16-byte chunk x is kept at x ^ swz(r): eight rows of K read at one chunk, or of V at two neighbours transposed (0..3 and 8..11 of 16), fall on
     // different banks.
-    const auto swz_k = [](int row) { return kD == 128 ? row & 7 : (row >> 2) & 1; };
-    const auto swz_v = [](int row) { return kD == 128 ? ((row >> 1) & 1) << 1 | ((row >> 3) & 1) << 2 : ((row >> 3) & 1) << 1; };
+    const auto swz_k = [](int row) { return !k8 ? Tile<kD>::swz_k(row) : kD == 128 ? row & 7 : (row >> 2) & 1; };
+    const auto swz_v = [](int row) { return !k8 ? Tile<kD>::swz_v(row) : kD == 128 ? ((row >> 1) & 1) << 1 | ((row >> 3) & 1) << 2 : ((row >> 3) & 1) << 1; };
     const unsigned int mine_at = lds_offset(mine), powers_at = lds_offset(powers);
     const auto token_of = [&](int it) __attribute__((always_inline)) { return pc.t0 + (stream + it * streams) * kTokens; };
     const auto issue = [&](const unsigned char *src, const auto &swz, int it, int part) __attribute__((always_inline)) {
@@ -46,14 +48,16 @@ __device__ __forceinline__ void attend_some(const ServeArgs &a, const ServePiece
       }
     };
     const auto issue_k = [&](int it) __attribute__((always_inline)) {     // the powers of two tokens a lane, and K
-      const int64_t x = pages.place(token_of(it)).token, y = pages.place(token_of(it) + 16).token;
-      global_to_lds_4(pages.powers + 2 * ((lane & 8) ? y : x) + 4 * (lane & 7), powers_at + (it & 1) * kPowers);
-      issue(pages.k, swz_k, it, 2 * (it & 1));
+      if constexpr (k8) {
+        const int64_t x = pages.place(token_of(it)).token, y = pages.place(token_of(it) + 16).token;
+        global_to_lds_4(pages.powers + 2 * ((lane & 8) ? y : x) + 4 * (lane & 7), powers_at + (it & 1) * kPowers);
+      }
+      issue(pages.k, swz_k, it, k8 ? 2 * (it & 1) : 0);
     };
-    const auto issue_v = [&](int it) __attribute__((always_inline)) { issue(pages.v, swz_v, it, 2 * (it & 1) + 1); };
+    const auto issue_v = [&](int it) __attribute__((always_inline)) { issue(pages.v, swz_v, it, k8 ? 2 * (it & 1) + 1 : 1); };
     issue_k(0);
     issue_v(0);
-    if (n > 1) {
+    if (k8 && n > 1) {
       issue_k(1);
       issue_v(1);
     }
@@ -62,7 +66,7 @@ __device__ __forceinline__ void attend_some(const ServeArgs &a, const ServePiece
 #pragma unroll
     for (int g = 0; g < kReads; ++g)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) q[g][i] = from[2 * (2 * g + h) + i];
+      for (int i = 0; i < 2; ++i) q[g][i] = from[k8 ? 2 * (2 * g + h) + i : 2 * (2 * g + i) + h];
     wait_loads<0>();
 #pragma unroll
     for (int g = 0; g < kReads; ++g) asm volatile("" : "+v"(q[g][0]), "+v"(q[g][1]));    // (waited for here, and not in the loop)
@@ -71,18 +75,25 @@ __device__ __forceinline__ void attend_some(const ServeArgs &a, const ServePiece
       int l64 = lane;
       if constexpr (kMasked) asm volatile("" : "+v"(l64));  // (worked out again in the last tiles: kept, there are too few registers)
       const int n32 = l64 & 31, h = l64 >> 5;
-      const int buf = it & 1, seen = last_seen - token_of(it) - 4 * h;
+      const int buf = k8 ? it & 1 : 0, seen = last_seen - token_of(it) - 4 * h;
       const bool more = it + 1 < n, more2 = it + 2 < n;
-      if (more) wait_loads<3 * kLoads + 1>();
+      if (k8 && more) wait_loads<3 * kLoads + 1>();
       else wait_loads<kLoads>();
       const unsigned char *K = mine + 2 * buf * kTileBytes, *V = K + kTileBytes, *P = powers + buf * kPowers;
       f32x16 s = (f32x16){0.f};
       u32x2 pv[4];                                         // K's and V's bytes of keys 8 j + 4 h + 0..3
 #pragma unroll
-      for (int j = 0; j < 4; ++j) pv[j] = *reinterpret_cast<const u32x2 *>(P + 16 * j + 8 * h);
-      const float power = power_of(P[2 * n32]);
+      for (int j = 0; j < 4; ++j)
+        if constexpr (k8) pv[j] = *reinterpret_cast<const u32x2 *>(P + 16 * j + 8 * h);
+      const float power = k8 ? power_of(P[2 * n32]) : 1.f;
 #pragma unroll
       for (int g = 0; g < kReads; ++g) {
+        if constexpr (!k8) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_b128(K + (k_at<kD>(l64) ^ (2 * g + i) << 5)), q[g][i], s, 0, 0, 0);
+          continue;
+        }
         const u32x4 codes = *reinterpret_cast<const u32x4 *>(K + n32 * kRow + (((2 * g + h) ^ swz_k(n32)) << 4));
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -91,7 +102,7 @@ __device__ __forceinline__ void attend_some(const ServeArgs &a, const ServePiece
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (more2) issue_k(it + 2);
+      if (k8 ? more2 : more) issue_k(it + (k8 ? 2 : 1));
       if constexpr (kMasked) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + (e & 3) <= seen ? s[e] : -INFINITY;
@@ -113,15 +124,17 @@ __device__ __forceinline__ void attend_some(const ServeArgs &a, const ServePiece
       for (int e = 0; e < 16; ++e) {
         const float p = fast_exp2((s[e] - m) * a.scale_log2);
         sum[e & 1] += p;
-        pb[e >> 3][e & 7] = (__bf16)(p * power_in(pv[e >> 2][(e & 3) >> 1], e, true));
+        pb[e >> 3][e & 7] = (__bf16)(k8 ? p * power_in(pv[e >> 2][(e & 3) >> 1], e, true) : p);
         if (kMasked) ones[e >> 3][e & 7] = (__bf16)(8 * (e >> 2) + (e & 3) <= seen ? 1.f : 0.f);
       }
       l += sum[0] + sum[1];
-      if (more2) wait_loads<3 * kLoads + 2>();
-      else if (more) wait_loads<2 * kLoads + 1>();
-      else wait_loads<0>();
+      if (!more) wait_loads<0>();
+      else if (!k8) wait_loads<kLoads>();
+      else if (more2) wait_loads<3 * kLoads + 2>();
+      else wait_loads<2 * kLoads + 1>();
       const int j = (l64 & 15) >> 1, of_16 = 4 * h + (j & 3) + 8 * (j >> 2), which = (l64 >> 4) & 1;
       const auto read_v = [&](int st, int db) __attribute__((always_inline)) {
+        if constexpr (!k8) return read_vt<kD>(V + (vt_at<kD>(l64) ^ db << 6), st);
         typedef __attribute__((ext_vector_type(2))) int i32x2;
         const int row = 16 * st + of_16;
         const i32x2 codes = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
@@ -142,7 +155,7 @@ __device__ __forceinline__ void attend_some(const ServeArgs &a, const ServePiece
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (more2) issue_v(it + 2);
+      if (k8 ? more2 : more) issue_v(it + (k8 ? 2 : 1));
     };
     int it = 0;
     for (; it < n_full; ++it) step(it, std::false_type());
@@ -173,7 +186,7 @@ __device__ __forceinline__ void attend_some(const ServeArgs &a, const ServePiece
       const int wave = (k << shift) + first;
       const float f = factor(ml[wave][n][0], top, a.scale_log2);
       ls = fmaf(ml[wave][n][1], f, ls);
-      sum += *reinterpret_cast<const f32x4 *>(lds + wave * 4 * kTileBytes + (n * kOut + (chunk ^ (n & (kOut - 1)))) * 16) * f;
+      sum += *reinterpret_cast<const f32x4 *>(lds + wave * kPlace + (n * kOut + (chunk ^ (n & (kOut - 1)))) * 16) * f;
     }
     if (!pc.direct) {
       *reinterpret_cast<f32x4 *>(a.part_o + (part + r) * kD + 4 * chunk) = sum;

@@ -34,8 +34,8 @@ def quantise(x):
 
 
 def wide_table(B, Hkv, d, page):
-    """Entries per request for which prefixes are read once, whatever the types: 2^27 bytes of one byte per element."""
-    return (1 << 27) // (B * page * 2 * Hkv * d) + 1
+    """Entries per request for which prefixes are read once, whatever the types: 200 MiB of one byte per element."""
+    return (200 << 20) // (B * page * 2 * Hkv * d) + 1
 
 
 class Shared:

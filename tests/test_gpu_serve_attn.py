@@ -59,7 +59,7 @@ def test_shared_prefixes(sp, dtype, cache, Hq, Hkv, d, kv, new, groups):
 def test_tables_of_either_side_of_the_rule(sp, dtype, cache):
     """Prefixes of tables that hold little are read request by request: the same result."""
     for kv, new in (([130, 240, 99], [1, 1, 1]), ([130, 240, 99], [9, 30, 2])):
-        width = {"f32": 1 << 25, "bf16": 1 << 27}[dtype] // (3 * 16 * 2 * 2 * 64 * (1 if cache == "e4m3" else 4 if dtype == "f32" else 2))
+        width = {"f32": 32 << 20, "bf16": 200 << 20}[dtype] // (3 * 16 * 2 * 2 * 64 * (1 if cache == "e4m3" else 4 if dtype == "f32" else 2))
         for w in (None, width, width + 1):
             _check(sp, s8.Shared(kv, new, [(0, 3, 96)], dtype=dtype, cache=cache, Hq=14, Hkv=2, d=64, seed=9, width=w, wide=False))
 
@@ -117,19 +117,20 @@ def test_tiles_that_some_rows_do_not_see_whole(sp, cache, d, kv, new):
         _check(sp, x)
 
 
+@pytest.mark.parametrize("cache", ["own", "e4m3"])
 @pytest.mark.parametrize("Hq, Hkv, d", [(28, 4, 128), (8, 8, 64), (8, 1, 128), (14, 2, 64)])
 @pytest.mark.parametrize("kv, new", [([1900, 700, 64], [3, 4, 1]), ([900], [8]), ([33, 17, 8, 0, 2], [8, 1, 8, 0, 2]), ([512, 96, 31], [8, 8, 8])])
-def test_chains_over_8_bits(sp, Hq, Hkv, d, kv, new):
+def test_chains(sp, cache, Hq, Hkv, d, kv, new):
     """17 to 64 rows a request and fewer; one new token's value a NaN at the end."""
     for more in (1, 4) if Hq == Hkv else (1,):             # (one query head a group: 4 to 32 tokens)
         n = [min(more * x, k) for x, k in zip(new, kv)]
-        x = s8.Shared(kv, n, cache="e4m3", Hq=Hq, Hkv=Hkv, d=d, page=16, seed=sum(kv), extra_rows=1)
-        _check(sp, x, groups=False)
+        x = s8.Shared(kv, n, cache=cache, Hq=Hq, Hkv=Hkv, d=d, page=16, seed=sum(kv), extra_rows=1)
+        _check(sp, x, groups=cache == "own")
         x.put(0, kv[0] - 2, V=float("nan"))
-        _check(sp, x, groups=False)
+        _check(sp, x, groups=cache == "own")
     for rows in (17, 32, 33, 64):
         if Hq // Hkv == 1:
-            _check(sp, s8.Shared([rows + 80, rows], [rows, rows], cache="e4m3", Hq=Hq, Hkv=Hkv, d=d, seed=rows, width=80), groups=False)
+            _check(sp, s8.Shared([rows + 80, rows], [rows, rows], cache=cache, Hq=Hq, Hkv=Hkv, d=d, seed=rows, width=80), groups=cache == "own")
 
 
 def test_exponents_of_any_byte(sp):

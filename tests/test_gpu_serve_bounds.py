@@ -67,7 +67,7 @@ def test_groups_that_no_batch_has(sp, dtype, cache):
 @pytest.mark.parametrize("dtype, cache", KINDS)
 def test_many_requests_of_all_rows(sp, dtype, cache):
     """Sixty requests that each claim every row, in groups or not: more blocks and pieces than the call has workgroups for."""
-    for new, width, groups in ((40, 200, 0), (300, 200, 0), (40, 20, 0), (40, 600, 8), (300, 600, 30), (40, 200, 8)):
+    for new, width, groups in ((40, 200, 0), (300, 200, 0), (40, 20, 0), (40, 900, 8), (300, 900, 30), (40, 200, 8)):
         x = s8.Shared([min(16 * width, 2500)] + [1] * 59, [new] + [0] * 59, dtype=dtype, cache=cache, Hq=14, Hkv=2, d=64, seed=new, width=width)
         x.kv_len = ref.ints([2000] * 60)
         if groups:

@@ -22,8 +22,8 @@ COVERAGE = {
     **{f"serve_few_kernel<{c}, 64, {w}>": (RA, "test_batches_of_every_size") for c in (BF16, E4M3) for w in (2, 4, 8)},
     **{f"serve_few_kernel<{c}, 128, {w}>": (RA, "test_batches_of_heads_of_128") for c in (BF16, E4M3) for w in (2, 4)},
     **{f"serve_few_kernel<{c}, 128, 8>": (RA, "test_long_contexts") for c in (BF16, E4M3)},
-    # 8 bits, 17 to 64 rows a request at most
-    **{f"serve_some_kernel<{d}>": (AT, "test_chains_over_8_bits") for d in (64, 128)},
+    # 17 to 64 rows a request at most
+    **{f"serve_some_kernel<{c}, {d}>": (AT, "test_chains") for c in (BF16, E4M3) for d in (64, 128)},
     # <storage type, head_dim, wavefronts that share a row's pieces>
     **{f"serve_combine_kernel<{t}, {d}, {n}>": (AT, "test_shared_prefixes") for t in (F32, BF16) for d in (64, 128) for n in (1, 2, 8)},
 }
