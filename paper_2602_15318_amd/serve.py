@@ -215,7 +215,8 @@ def chunk_attn8(q, k_cache, v_cache, exponents, block_table, cu_new, kv_len, max
 def prefix_attn(q, k_cache, v_cache, block_table, cu_new, kv_len, group_start, prefix_len, max_new: int, exponents=None, scale: float = 0.0,
                 out=None, lse=None, want_lse: bool = True, workspace=None, stream=None):
     """sparrow_prefix_attn.  chunk_attn's arguments, and group_start int32 [G+1], prefix_len int32 [G] on the GPU: requests group_start[g]
-    to group_start[g+1]-1 begin with the same prefix_len[g] tokens, which are read once for all of them.  An 8-bit cache comes with its
+    to group_start[g+1]-1 begin with the same prefix_len[g] tokens, which are read once for all of them.  (Request by request where the tables
+    hold so little that this is faster; the result is the same.)  An 8-bit cache comes with its
     exponents, another is of q's dtype.  Returns (out, lse); rows behind cu_new[B] are left as they were."""
     r = _native.prefix_attn(q, k_cache, v_cache, block_table, cu_new, kv_len, group_start, prefix_len, max_new, exponents, scale, out, lse,
                             want_lse, workspace, stream)
