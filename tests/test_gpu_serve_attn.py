@@ -87,6 +87,7 @@ def test_many_requests_and_groups(sp, cache):
     kv = [65 + b % 40 for b in range(256)]
     _check(sp, s8.Shared(kv, [1 + b % 3 for b in range(256)], [(4 * g, 4 * g + 4, 20 + g) for g in range(40)], cache=cache, Hq=4, Hkv=2, d=64, seed=2))
     _check(sp, s8.Shared(kv, [1] * 256, [(0, 256, 60)], cache=cache, Hq=8, Hkv=1, d=128, seed=3))
+    _check(sp, s8.Shared([b + 90 for b in kv], [b % 2 for b in range(256)], [(4 * g, 4 * g + 4, 130) for g in range(64)], cache=cache, Hq=2, Hkv=1, d=64, seed=4))
 
 
 def test_values_that_are_no_numbers_stay_where_they_are_seen(sp):

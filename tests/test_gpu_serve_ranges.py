@@ -92,6 +92,26 @@ def test_a_workspace_for_calls_one_after_the_other(sp):
             assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("dtype, cache", KINDS)
+def test_pages_beyond_32_bits(sp, dtype, cache):
+    """Pages more than 2^32 bytes behind the first, one token, a chain, a chunk and a shared prefix, and read back."""
+    kind = torch.float8_e4m3fn if cache == "e4m3" else ref.DT[dtype]
+    far = (3 << 29) // kind.itemsize                       # elements between pages: 1.5 GiB
+    bufs = [torch.empty(far * 5 + (1 << 16), dtype=kind, device="cuda") for _ in range(2)]
+    for kv, new, groups in (([40], [1], []), ([40], [3], []), ([40], [20], []), ([40, 30], [2, 9], [(0, 2, 20)])):
+        x = s8.Shared(kv, new, groups, dtype=dtype, cache=cache, Hq=7, Hkv=1, d=128, page=32, seed=sum(new))
+        n = x.k.shape[0]
+        assert 4 <= n <= 6 and (n - 1) * far * kind.itemsize > 1 << 32
+        views = [torch.as_strided(b, x.k.shape, (far, 128, 128, 1)) for b in bufs]
+        for view, t in zip(views, (x.k, x.v)):
+            view.view(torch.uint8).copy_(t.view(torch.uint8))
+        x.k, x.v = views
+        _check(sp, x, groups=bool(groups) or cache == "own")
+        out = [torch.empty((kv[0], 1, 128), dtype=ref.DT[dtype], device="cuda") for _ in range(2)]
+        sp.page_gather(x.k, x.v, x.table[:1], ref.ints([0, kv[0]]), *out, exponents=x.exps)
+        assert torch.equal(out[0], x.K[0]) and torch.equal(out[1], x.V[0])
+
+
 def test_offsets_of_rows_beyond_32_bits(sp):
     """Query rows that lie more than 2^31 elements apart from the first."""
     row = 1 << 20
