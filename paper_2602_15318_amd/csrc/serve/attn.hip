@@ -11,10 +11,10 @@ hipError_t launch_serve_f32(int d, int pieces, const ServeArgs &a, hipStream_t s
 hipError_t launch_serve_combine(int dtype, int d, const ServeArgs &a, hipStream_t st);
 
 // The plan, blocks that are partly filled and a second pass over all rows cost 5 to 9 us, and what a group's requests read of one prefix comes out of the
-// caches: below these sizes every request reads its own.  bf16, shared and not, us: 8 of 2,100 tokens (34 MB) 19.5 and 14.2; 4 of 8,500 (70 MB) 22.6 and
-// 18.3; 8 of 8,300 (137 MB) 24.3 and 23.5, with four query heads and one KV head 23.1 and 25.0; 3 chains of 26,300 (161 MB) 37.5 and 29.3; 12 chains of 8,300
-// (206 MB) 40.1 and 35.0; 32 of 3,100 (206 MB) 29.0 and 23.8; 16 of 8,300 (275 MB) 27.0 and 39.0; 64 of 2,200 (288 MB) 32.1 and 29.2; 8 of 26,300 (430 MB) 28.4
-// and 59.6.  fp32: 4 of 2,060 (34 MB) 21.5 and 21.3; 8 (68 MB) 22.5 and 26.4.
+// caches: below these sizes every request reads its own.  bf16, shared and not, us: 8 of 2,100 tokens (34 MB) 19.0 and 13.1; 4 of 8,500 (70 MB) 22.6 and
+// 17; 8 of 8,300 (137 MB) 23.5 and 19.2, with four query heads and one KV head 22.3 and 18.8; 3 chains of 26,300 (161 MB) 37.5 and 29.3; 12 chains of 8,300
+// (206 MB) 40.1 and 35.0; 32 of 3,100 (206 MB) 28.5 and 22.2; 16 of 8,300 (275 MB) 26.6 and 26.5, with 8 KV heads of 64 22.7 and 30.7; 64 of 2,200 (288 MB)
+// 32.1 and 27.3; 8 of 26,300 (430 MB) 28.9 and 36.2; 32 of them 41.6 and 97.  fp32: 4 of 2,060 (34 MB) 21.5 and 21.3; 8 (68 MB) 22.5 and 26.4.
 bool serve_shares(int dtype, int64_t tokens, int64_t bytes) { return tokens > (dtype == SPARROW_F32 ? 32ll << 20 : 200ll << 20) / bytes; }
 
 ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t n_rows, int max_new, int64_t capacity) {

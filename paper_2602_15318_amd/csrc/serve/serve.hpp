@@ -42,6 +42,7 @@ struct ServeArgs {
   int64_t table_stride, q_row, stride_page, stride_token, stride_head;          // elements
   int32_t B, G, n_rows, max_new, Hq, Hkv, g, table_width, page_shift, n_pages;
   int32_t block_shift;     // log2 of the rows of a block
+  int32_t once;            // no page is another request's too, as far as is known
   int32_t slots, round;    // pieces per KV head at most (0: nothing is cut or shared, one piece a block); those that run at once
   float scale_log2, inv_g;
   float *part_o, *part_ml; // [piece * Hkv + KV head][row of the block]: unnormalised output [d]; reference score, sum
