@@ -118,6 +118,21 @@ def test_tiles_that_some_rows_do_not_see_whole(sp, cache, d, kv, new):
         _check(sp, x)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kv, new", [(96, 90), (400, 70), (128, 8)])
+def test_a_code_times_its_power_beyond_all_numbers(sp, d, kv, new):
+    """In the last token, which only the last row sees: the rows before it are as without."""
+    x = s8.Shared([kv], [new], cache="e4m3", Hq=14, Hkv=2, d=d, seed=12)
+    o, l, tol, ltol = ref.attention(x)
+    page, t = int(x.table[0, (kv - 1) // 16]), (kv - 1) % 16
+    for which, cache in enumerate((x.k, x.v)):
+        cache.view(torch.uint8)[page, t] = 0x7e
+        x.exps[page, :, t, which] = 254
+    out, lse = x.attend(sp, groups=False)
+    ref.close(out[:new - 1], o[:new - 1], tol[:new - 1])
+    ref.close(lse[:new - 1], l[:new - 1], ltol[:new - 1])
+
+
 @pytest.mark.parametrize("cache", ["own", "e4m3"])
 @pytest.mark.parametrize("Hq, Hkv, d", [(28, 4, 128), (8, 8, 64), (8, 1, 128), (14, 2, 64)])
 @pytest.mark.parametrize("kv, new", [([1900, 700, 64], [3, 4, 1]), ([900], [8]), ([33, 17, 8, 0, 2], [8, 1, 8, 0, 2]), ([512, 96, 31], [8, 8, 8])])
