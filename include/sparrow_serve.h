@@ -13,8 +13,11 @@
  * power of two for the row of K and one for that of V:
  *     element = code * 2^(byte - 127),   byte at exponents[((page * Hkv + head) * page_size + token of the page) * 2 + (0: K, 1: V)]
  * It is written with the smallest power, 2^-100 at least, for which no finite element of the row passes 448; a code is the e4m3 number nearest
- * to the element, ties to even.  An infinite or NaN element becomes NaN.  A held element is a bf16 number: reading it back rounds nothing.
- * The strides of such a cache count bytes.  Contents are not trusted: a byte above 254 or below 1 is taken as the nearest of these.
+ * to the element, ties to even.  An infinite or NaN element (also one of K that its rotation takes beyond fp32) becomes NaN.  So bytes from 27 to 247 are
+ * written, and a held element is a bf16 number that is read back without a rounding, or 2^128, which elements from 248 * 2^120 (3.3e38) on round to
+ * and which is read back as infinite.
+ * The strides of such a cache count bytes.  Contents are not trusted: a byte above 254 or below 1 is taken as the nearest of these, by the attention
+ * one of V below 9 as 9.  Of powers that are not written, elements below 2^-133 are no bf16 numbers, and those from 2^128 on are infinite.
  */
 #ifndef SPARROW_SERVE_H
 #define SPARROW_SERVE_H
@@ -55,6 +58,7 @@ int sparrow_page_gather(const sparrow_paged_desc *desc, const void *k_cache, con
 /*
  * sparrow_chunk_attn over an 8-bit cache: its arguments, and exponents behind the caches.  The workspace is
  * sparrow_prefix_attn_workspace()'s for n_groups = 0.
+ * The output is finite where the sum of the elements that a row sees, each times its weight about the largest score (1 at most), is a number of fp32.
  */
 int sparrow_chunk_attn8(const sparrow_paged_desc *desc, const void *q, const void *k_cache, const void *v_cache,
                         const uint8_t *exponents, const int32_t *block_table, int32_t table_width, int64_t table_stride,
@@ -68,7 +72,8 @@ int sparrow_chunk_attn8(const sparrow_paged_desc *desc, const void *q, const voi
  * Where the tables of the batch hold little (B * table_width * page_size tokens of 200 MiB of K and V of all heads at most, 32 MiB for fp32), a plan
  * for groups costs more than it saves, and every request reads its own: n_groups changes nothing then.
  *
- *  exponents    dev uint8 of an 8-bit cache; NULL: the cache is of desc->dtype
+ *  exponents    dev uint8 of an 8-bit cache; NULL: the cache is of desc->dtype (the weights then reach 2^8, as in sparrow_chunk_attn: elements of V above
+ *               2^119 can pass fp32 in a product or a sum, the output is infinite or NaN then)
  *  block_table  every request's row holds its whole context.  The prefix is read through the row of the group's first request that has new
  *               tokens; the tokens behind it through each request's own.  Whole pages of a prefix are usually the same pages in all rows.
  *  group_start  dev int32 [n_groups+1] ascending, from 0 to B; requests outside all groups share nothing.  NULL where n_groups = 0

@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) serve_attn_f32_kernel(ServeArg
 #pragma unroll
     for (int db = 0; db < kDB; ++db) {
       f32x4 x = {0.f, 0.f, 0.f, 0.f};
-      if (!none) x = o[db] / l;
+      if (!none) x = o[db] / (k8 ? l * kLowered : l);
       *reinterpret_cast<f32x4 *>((float *)a.out + to * kD + 16 * db + 4 * c4) = x;
     }
     if (a.lse && c4 == 0) a.lse[to] = none ? -INFINITY : log_sum(m, a.scale_log2, l);

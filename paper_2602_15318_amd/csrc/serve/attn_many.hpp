@@ -333,7 +333,7 @@ __device__ __forceinline__ void attend_many(const ServeArgs &a, const ServePiece
   if (pc.direct) {
     const bool none = pc.it.past + i_row < 0;
     const int64_t to = (int64_t)(pc.it.row0 + i_row) * a.Hq + head;
-    const float inv = none ? 0.f : near / l;
+    const float inv = none ? 0.f : near / (k8 ? l * kLowered : l);
 #pragma unroll
     for (int db = 0; db < kDB; ++db)
 #pragma unroll

@@ -200,7 +200,7 @@ __device__ __forceinline__ void attend_some(const ServeArgs &a, const ServePiece
     const int64_t at = (int64_t)(pc.it.row0 + i) * a.Hq + c * a.g + r - i * a.g;
     const bool none = pc.it.past + i < 0;
     if (none) sum = (f32x4){0.f, 0.f, 0.f, 0.f};
-    else sum /= ls;
+    else sum /= k8 ? ls * kLowered : ls;
     *reinterpret_cast<u32x2 *>((bf16_t *)a.out + at * kD + 4 * chunk) = (u32x2){pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3])};
     if (a.lse && chunk == 0) a.lse[at] = none ? -INFINITY : log_sum(top, a.scale_log2, ls);
   }

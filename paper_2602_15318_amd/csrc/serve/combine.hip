@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(64 * (kSpread == 1 ? 4 : kSpread)) serve_combi
     }
     const int64_t to = (int64_t)r * a.Hq + h;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    if (!none) x = st.o / st.l;
+    if (!none) x = st.o / (st.l * lowered(a));
     if constexpr (sizeof(T) == 4)
       *(f32x4 *)((float *)a.out + to * kD + at4) = x;
     else

@@ -63,4 +63,9 @@ hipError_t launch_serve_attn(int dtype, int d, const ServeShape &s, const ServeA
 // 2^(byte - 127) of a row of an 8-bit cache, normal and finite whatever the byte
 __device__ __forceinline__ float power_of(unsigned int byte) { return __uint_as_float(min(max(byte, 1u), 254u) << 23); }
 
+// Weights reach 2^8 (kSlack): beside an 8-bit cache the attention's outputs are kept, in partials too, times this, so that a weight times a power, or
+// times an element, is finite where the element is.  What divides by the weights' sum puts it right, exactly.
+constexpr float kLowered = 0x1p-8f;
+__device__ __forceinline__ float lowered(const ServeArgs &a) { return a.exponents ? kLowered : 1.f; }
+
 }  // namespace sparrow

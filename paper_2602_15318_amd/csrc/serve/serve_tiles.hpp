@@ -40,9 +40,10 @@ template <typename C> __device__ __forceinline__ ServePages<C> serve_pages(const
   return p;
 }
 
-// K's, or V's, power of row `row` from the four bytes of it and its neighbour
+// K's, or V's, power of row `row` from the four bytes of it and its neighbour.  V's is kLowered (serve.hpp) below what stands there: finite times any weight.
 __device__ __forceinline__ float power_in(unsigned int bytes, int row, bool is_v) {
-  return power_of((bytes >> (16 * (row & 1) + (is_v ? 8 : 0))) & 0xffu);
+  const unsigned int byte = (bytes >> (16 * (row & 1) + (is_v ? 8 : 0))) & 0xffu;
+  return is_v ? __uint_as_float((min(max(byte, 9u), 254u) - 8u) << 23) : power_of(byte);
 }
 // Four codes times a power of two, exactly, as four bf16
 __device__ __forceinline__ u32x2 four_of(unsigned int codes, float power) {
