@@ -33,7 +33,10 @@ ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t 
   const int at_once = f32 ? (d == 128 ? 512 : 1024) : G == 0 && s.rows == 16 ? 2048 / s.waves : 256;       // workgroups
   s.round = std::max(at_once / Hkv, 1);
   if (G > 0) {
-    s.slots = (int)std::max<int64_t>(4 * s.round, blocks);
+    // Two rounds of pieces beside the blocks, one of which every request has: the plan tries to cut some 0.5 to 2.4 rounds off.  us where the blocks were counted
+    // among the four rounds, and now, single tokens over a shared 26,112, heads of 128, bf16: 28 and 4 heads, 224 requests 152 and 128, 240 517 and 134,
+    // 256 516 and 139; 32 and 8, 112 92 and 92, 124 512 and 95, 256 517 and 172; 32 of each, 32 404 and 117.  (Half a round: 256 over 8 bits 143 -> 151.)
+    s.slots = (int)std::max<int64_t>(4 * s.round, blocks + 2 * s.round);
   } else if (most <= s.rows) {
     s.round = std::max(s.round, 2 * B);                    // (256 of up to 3,000 tokens 99.5 us, of B + 1 pieces 110, of 4 B 104)
     // Requests of up to 512 tokens (fp32: 128), 1,024 where they fill half of the chip, in one piece each and without a second pass, by what the tables

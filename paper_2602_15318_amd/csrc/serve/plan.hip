@@ -67,7 +67,7 @@ __device__ __forceinline__ int best_piece(const ServeArgs &a, Plan *p, int items
     const float rounds = __builtin_ceilf(wave_sum_valu(big) * inv_round);
     const float cost = fmaxf(wave_sum_valu(sum) * inv_round + kRest * most, rounds * most) + kCombine * (float)a.Hkv * wave_sum_valu(ends);
     if (lane == 0) {
-      p->cost[w] = N > a.slots && N > U ? 3.4e38f : cost;              // (uncut blocks always fit)
+      p->cost[w] = N > a.slots && N > U ? 3.4e38f : cost;              // (uncut blocks always fit, and half a round more: the first way)
       p->T[w] = T;
     }
   }

@@ -1,0 +1,71 @@
+"""The pieces that large batches are cut into, as the plan leaves them in the workspace, and that the results are the same either way."""
+import pytest
+import torch
+
+import paged_ref as ref
+
+pytestmark = pytest.mark.gpu
+D, PAGE = 128, 64
+
+
+@pytest.fixture(scope="module")
+def sp():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2602_15318_amd as sp_
+    return sp_
+
+
+class Many:
+    """Requests of kv tokens, the last `new` of them new, on pages of their own behind `prefix` (whole pages) that all of them share."""
+
+    def __init__(self, kv, new, prefix, Hq, Hkv, dtype=torch.bfloat16, seed=0):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        B, whole = len(kv), prefix // PAGE
+        own = [-(-k // PAGE) - whole for k in kv]
+        n = whole + sum(own)
+        ids = torch.randperm(n, generator=g, device="cuda").to(torch.int32)
+        self.table = torch.full((B, whole + max(own)), -1, dtype=torch.int32, device="cuda")
+        at = whole
+        for b in range(B):
+            self.table[b, :whole] = ids[:whole]
+            self.table[b, whole:whole + own[b]] = ids[at:at + own[b]]
+            at += own[b]
+        self.k, self.v = (torch.randn((n, PAGE, Hkv, D), generator=g, device="cuda").to(dtype) for _ in range(2))
+        cu = [0]
+        for m in new:
+            cu.append(cu[-1] + m)
+        self.q = torch.randn((cu[-1], Hq, D), generator=g, device="cuda").to(dtype)
+        self.cu, self.kv_len, self.start, self.prefix, self.max_new = ref.ints(cu), ref.ints(kv), ref.ints([0, B]), ref.ints([prefix]), max(new)
+
+    def attend(self, sp, groups):
+        """out, lse, the workspace"""
+        B, G = self.kv_len.shape[0], int(groups)
+        ws = torch.zeros(sp.prefix_attn_workspace_bytes(self.q, self.k, self.v, B, G, self.max_new), dtype=torch.uint8, device="cuda")
+        start, prefix = (self.start, self.prefix) if groups else (None, None)
+        return *sp.prefix_attn(self.q, self.k, self.v, self.table, self.cu, self.kv_len, start, prefix, self.max_new, workspace=ws), ws
+
+
+@pytest.mark.parametrize("Hq, Hkv, B", [(28, 4, 32), (28, 4, 224), (28, 4, 256), (32, 8, 112), (32, 8, 128), (32, 8, 256), (32, 32, 32), (32, 32, 64)])
+def test_a_shared_prefix_is_spread_whatever_the_batch(sp, Hq, Hkv, B):
+    """The pieces of the prefix, of all KV heads, are 96 at least (uncut they would be 16 to 32): beside the requests' own, for a chip of 256."""
+    prefix = 12_800
+    x = Many([prefix + 20 + b for b in range(B)], [1] * B, prefix, Hq, Hkv)
+    out, lse, ws = x.attend(sp, True)
+    rows = 64 if B * Hq // Hkv <= 64 else 256             # of a block
+    each = Hkv * rows * (D + 2) * 4 + 48     # a piece's partials and its 12 whole numbers, which are last
+    slots = (ws.numel() - 32 * B) // each
+    ends = ws.numel() - -(-slots * 48 // 256) * 256
+    n = int(ws[ends - 256:ends - 252].view(torch.int32))
+    assert 0 < n <= slots
+    pieces = ws[ends:ends + 48 * n].view(torch.int32).view(n, 12).cpu()
+    of_prefix = pieces[(pieces[:, 3] == 0) & (pieces[:, 4] == prefix)]       # first key and end of the item
+    assert len(of_prefix) * Hkv >= 96
+    # every block of the prefix is covered once
+    blocks = -(-B * Hq // Hkv // rows)
+    for block in range(blocks):
+        t = sorted((int(p[7]), int(p[8])) for p in of_prefix if int(p[6]) == block)
+        assert t[0][0] == 0 and t[-1][1] == prefix and all(a[1] == b[0] for a, b in zip(t, t[1:]))
+    # bf16 weights and outputs are rounded once each: half a step 2^-8 of the sizes on either side, sums of p |v| below 4 for N(0, 1)
+    want, want_lse, _ = x.attend(sp, False)
+    assert (out.double() - want.double()).abs().max() <= 4 * 2 * 2.0 ** -8
+    assert (lse - want_lse).abs().max() <= 2e-4
