@@ -32,6 +32,7 @@ ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t 
   s.waves = B * Hkv <= 48 ? 8 : B * Hkv < 192 ? 4 : 2;
   const int at_once = f32 ? (d == 128 ? 512 : 1024) : G == 0 && s.rows == 16 ? 2048 / s.waves : 256;       // workgroups
   s.round = std::max(at_once / Hkv, 1);
+  s.ways = 1;
   if (G > 0) {
     // Two rounds of pieces beside the blocks, one of which every request has: the plan tries to cut some 0.5 to 2.4 rounds off.  us where the blocks were counted
     // among the four rounds, and now, single tokens over a shared 26,112, heads of 128, bf16: 28 and 4 heads, 224 requests 152 and 128, 240 517 and 134,
@@ -47,8 +48,12 @@ ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t 
     // Cut where the blocks fill two thirds of the chip at most; two rounds of pieces if they end sooner.  8 bits over 26,112 tokens, four KV heads of 128, us
     // cut and not: 1,000 new tokens 357 and 644, 1,500 511 and 645, 1,700 694 and 645.  Nothing is cut off two tiles: 100 over 100 21.7 and 19.3, with heads
     // of 64 18.3 and 11.4; 75 over 300 23.3 and 23.9, 17.9 and 18.9.
+    // A round of pieces at least beside the blocks, one of which every request has.  us where those took the place of the chunk's pieces, and now, a chunk of
+    // 512 over 26,112 beside single tokens over up to 4,000, 8 bits, heads of 128: 28 and 4 heads, 63 of them 203 and 207, 95 322 and 233, 109 614 and 233,
+    // 255 614 and 300; 32 and 8, 32 243 and 244, 47 322 and 260, 63 612 and 270, 255 615 and 430; beside 119 chains of 3, bf16, 514 and 310.
     const int64_t filled = (n_rows * g + s.rows - 1) / s.rows;
-    s.slots = capacity > 128 && 3 * filled <= 2 * s.round ? 2 * s.round : 0;
+    s.ways = 3;
+    s.slots = capacity > 128 && 3 * filled <= 2 * s.round ? (int)std::max<int64_t>(2 * s.round, blocks + s.round) : 0;
   }
   s.grid = (int)std::max<int64_t>(s.slots, G > 0 ? 0 : blocks);
   const int64_t units = (int64_t)s.slots * Hkv * s.rows;

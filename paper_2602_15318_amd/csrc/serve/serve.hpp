@@ -44,15 +44,16 @@ struct ServeArgs {
   int32_t block_shift;     // log2 of the rows of a block
   int32_t once;            // no page is another request's too, as far as is known
   int32_t slots, round;    // pieces per KV head at most (0: nothing is cut or shared, one piece a block); those that run at once
+  int32_t ways;            // ways to cut that a plan without groups tries (serve_plan.hpp)
   float scale_log2, inv_g;
   float *part_o, *part_ml; // [piece * Hkv + KV head][row of the block]: unnormalised output [d]; reference score, sum
   ServeLeft *left;         // [B]; NULL where slots is 0
   ServePiece *pieces;      // with groups: [slots], n_pieces of them
   int32_t *n_pieces;
 };
-// How a call of these sizes is run: rows per block, wavefronts per workgroup (16 rows), pieces per KV head at most, those that run at once, workgroups per KV head, floats of part_o and part_ml.
+// How a call of these sizes is run: rows per block, wavefronts per workgroup (16 rows), pieces per KV head at most, those that run at once, ways to cut, workgroups per KV head, floats of part_o and part_ml.
 struct ServeShape {
-  int rows, waves, slots, round, grid;
+  int rows, waves, slots, round, ways, grid;
   int64_t floats_o, floats_ml;
 };
 // Whether prefixes are read once for their groups, by the tokens that the tables of the batch hold and the bytes of one token's keys and values.

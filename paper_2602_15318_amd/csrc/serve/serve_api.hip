@@ -139,7 +139,7 @@ int attention(const sparrow_paged_desc *desc, const void *q, const void *k_cache
   a.G = serve_shares(desc->dtype, B * capacity, 2ll * a.Hkv * desc->head_dim * (exponents ? 1 : desc->dtype == SPARROW_F32 ? 4 : 2)) ? n_groups : 0;
   a.once = n_groups == 0 || a.G > 0;
   const ServeShape shape = serve_shape(desc->dtype, desc->head_dim, a.Hq, a.Hkv, B, a.G, n_rows, max_new, capacity);
-  a.slots = shape.slots; a.round = shape.round; a.block_shift = shift_of(shape.rows);
+  a.slots = shape.slots; a.round = shape.round; a.ways = shape.ways; a.block_shift = shift_of(shape.rows);
   a.part_o = (float *)workspace;
   a.part_ml = (float *)((unsigned char *)workspace + round_up((size_t)shape.floats_o * 4, 256));
   a.left = shape.slots == 0 ? nullptr : (ServeLeft *)((unsigned char *)a.part_ml + round_up((size_t)shape.floats_ml * 4, 256));

@@ -38,9 +38,10 @@ __device__ __forceinline__ void cut(ServePiece *q, int split, int n_splits) {
 }
 
 // Without groups; piece number `idx` of a KV head, false: there are not that many.  Blocks count down: the last, whose rows see most, come first.  T is the
-// smallest for which the heavy pieces, those of more than 16 rows where there are such, are not more than N, of one round of pieces or two that which
-// should end first; a piece's beginning and end take about `extra` grains.  Light ones end soon and fit in between: with all of them counted, batches
-// of a chunk and single tokens took 82 us instead of 74 (777 + 8 tokens, heads of 64) and 123 instead of 104 (512 + 16, heads of 128).
+// smallest for which the heavy pieces, those of more than 16 rows where there are such, are not more than N, of a.ways ways that which should end first: one
+// round of pieces, two, or one beside the blocks (where those alone take half a round: short requests fill the places, the time is the mean work and
+// then the longest piece); a piece's beginning and end take about `extra` grains.  Light ones end soon and fit in between: with all of them counted, batches of a chunk and single
+// tokens took 82 us instead of 74 (777 + 8 tokens, heads of 64) and 123 instead of 104 (512 + 16, heads of 128).
 __device__ __forceinline__ bool serve_find_piece(const ServeArgs &a, int idx, ServePiece *out) {
   const int lane = threadIdx.x & 63, most = a.table_width << a.page_shift;
   ServeItem rq[kMaxPerLane];                               // lane l's requests l, l + 64, ...
@@ -73,8 +74,8 @@ __device__ __forceinline__ bool serve_find_piece(const ServeArgs &a, int idx, Se
   const int U = lane_value(wave_scan(blocks), 63), H = lane_value(wave_scan(heavy), 63), extra = a.block_shift == 8 ? 2 : 4;
   const float W = wave_sum_valu(weight), V = wave_sum_valu(heavy_weight);
   int T = 1 << 29, best = 1 << 30;
-  for (int round = 1; round * a.round <= a.slots && U < a.slots; ++round) {
-    const int N = round * a.round;
+  for (int way = 1; way <= (2 * H > a.round ? a.ways : min(a.ways, 2)) && U < a.slots; ++way) {
+    const int N = way < 3 ? way * a.round : H + a.round;
     if (N <= H) continue;
     const auto grains = [&](float t) { return (min((int)(t * (1.f + 0x1p-14f)), 1 << 28) + kGrain) / kGrain; };
     int hi = max(grains(V / (float)(N - H)), grains(W / (float)(a.slots - U)));           // always fits
@@ -94,7 +95,7 @@ __device__ __forceinline__ bool serve_find_piece(const ServeArgs &a, int idx, Se
         else lo = mid;
       }
     }
-    const int cost = round * (hi + extra);
+    const int cost = way < 3 ? way * (hi + extra) : hi + extra + grains(V / (float)a.round);
     if (cost < best) {
       best = cost;
       T = hi * kGrain;

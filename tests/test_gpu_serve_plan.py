@@ -69,3 +69,24 @@ def test_a_shared_prefix_is_spread_whatever_the_batch(sp, Hq, Hkv, B):
     want, want_lse, _ = x.attend(sp, False)
     assert (out.double() - want.double()).abs().max() <= 4 * 2 * 2.0 ** -8
     assert (lse - want_lse).abs().max() <= 2e-4
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("Hq, Hkv, B, others", [(28, 4, 17, 1), (28, 4, 128, 1), (28, 4, 256, 1), (32, 8, 17, 1), (32, 8, 64, 1), (32, 8, 256, 1), (28, 4, 120, 3),
+                                                (32, 8, 60, 5)])
+def test_a_chunk_is_spread_whatever_the_batch(sp, dtype, Hq, Hkv, B, others):
+    """A chunk of 512 tokens (fp32 128) over 12,800, in workgroups for half of the chip at least, beside single tokens or chains over 200."""
+    f32, L = dtype == torch.float32, 12_800
+    chunk = 128 if f32 else 512
+    x = Many([L] + [200] * (B - 1), [chunk] + [others] * (B - 1), 0, Hq, Hkv, dtype)
+    out, lse, ws = x.attend(sp, False)
+    left = ws[ws.numel() - -(-B * 32 // 256) * 256:][:32 * B].view(torch.int32).view(B, 8).cpu()     # first piece, pieces of a block, ...
+    assert int(left[0, 1]) * -(-chunk * Hq // Hkv // (64 if f32 else 256)) * Hkv >= 128
+    # against the chunk and some of the others by themselves: bf16 weights and outputs are rounded once each, half a step 2^-8 of the sizes on either
+    # side, sums of p |v| below 4 for N(0, 1); fp32 sums of 12,800 wander by 2^-24 a term: 2^-14 is many times that
+    tol = 2.0 ** -14 if f32 else 4 * 2 * 2.0 ** -8
+    cu = x.cu.cpu().tolist()
+    for b in (0, 1, B // 2, B - 1):
+        rows = slice(cu[b], cu[b + 1])
+        want, want_lse = sp.prefix_attn(x.q[rows], x.k, x.v, x.table[b:b + 1], ref.ints([0, cu[b + 1] - cu[b]]), x.kv_len[b:b + 1], None, None, x.max_new)
+        assert (out[rows].double() - want.double()).abs().max() <= tol and (lse[rows] - want_lse).abs().max() <= 2e-4

@@ -16,7 +16,7 @@ def _slots(Hq, Hkv, B, G, n_rows, max_new, block_rows):
     d = serve.PagedDesc(**{**GOOD, "n_q_heads": Hq, "n_kv_heads": Hkv, "q_stride_row": Hq * D})
     total = int(serve.lib.sparrow_prefix_attn_workspace(ctypes.byref(d), B, G, n_rows, max_new))
     each = Hkv * block_rows * (D + 2) * 4 + (48 if G else 0)
-    assert 0 < (total - 32 * B) % each < 2048
+    assert 0 <= (total - 32 * B) % each < 2048
     return (total - 32 * B) // each
 
 
@@ -28,3 +28,14 @@ def test_prefixes_have_room_beside_the_requests(Hq, Hkv):
                 continue                     # (blocks of 64 rows)
             blocks = B * -(-new * Hq // Hkv // 256) + -(-B * new * Hq // Hkv // 256)
             assert _slots(Hq, Hkv, B, 1, B * new, new, 256) >= blocks + 2 * (256 // Hkv), (B, new)
+
+
+@pytest.mark.parametrize("Hq, Hkv", [(28, 4), (32, 8), (32, 32), (8, 1)])
+def test_chunks_have_room_beside_single_tokens(Hq, Hkv):
+    for B in range(2, 257):
+        for chunk in (130, 512):
+            g, n_rows = Hq // Hkv, chunk + B - 1
+            if chunk * g <= 256 or 3 * -(-n_rows * g // 256) > 2 * (256 // Hkv):
+                continue                     # (a block each, of which there is room for two; blocks that fill the chip)
+            blocks = -(-chunk * g // 256) + B - 1
+            assert _slots(Hq, Hkv, B, 0, n_rows, chunk, 256) >= blocks + 256 // Hkv, (B, chunk)
