@@ -69,8 +69,9 @@ int sparrow_chunk_attn8(const sparrow_paged_desc *desc, const void *q, const voi
  * sparrow_chunk_attn for requests that share prefixes: requests group_start[g] .. group_start[g+1]-1 of the batch begin with the same
  * prefix_len[g] tokens, and each group's prefix is read once for the new tokens of all its requests.  out and lse are what
  * sparrow_chunk_attn gives for the same tables.
- * Where the tables of the batch hold little (B * table_width * page_size tokens of 200 MiB of K and V of all heads at most, 32 MiB for fp32), a plan
- * for groups costs more than it saves, and every request reads its own: n_groups changes nothing then.
+ * Where the tables of the batch hold little (B * table_width * page_size tokens of 200 MiB of K and V of all heads at most, 32 MiB for fp32; over 8 bits
+ * from 80 and 16 MiB on, by the query rows of a request), a plan for groups costs more than it saves, and every request reads its own: n_groups changes nothing
+ * then.
  *
  *  exponents    dev uint8 of an 8-bit cache; NULL: the cache is of desc->dtype (the weights then reach 2^8, as in sparrow_chunk_attn: elements of V above
  *               2^119 can pass fp32 in a product or a sum, the output is infinite or NaN then)

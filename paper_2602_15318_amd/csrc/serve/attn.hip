@@ -15,7 +15,21 @@ hipError_t launch_serve_combine(int dtype, int d, const ServeArgs &a, hipStream_
 // 17; 8 of 8,300 (137 MB) 23.5 and 19.2, with four query heads and one KV head 22.3 and 18.8; 3 chains of 26,300 (161 MB) 37.5 and 29.3; 12 chains of 8,300
 // (206 MB) 40.1 and 35.0; 32 of 3,100 (206 MB) 28.5 and 22.2; 16 of 8,300 (275 MB) 26.6 and 26.5, with 8 KV heads of 64 22.7 and 30.7; 64 of 2,200 (288 MB)
 // 32.1 and 27.3; 8 of 26,300 (430 MB) 28.9 and 36.2; 32 of them 41.6 and 97.  fp32: 4 of 2,060 (34 MB) 21.5 and 21.3; 8 (68 MB) 22.5 and 26.4.
-bool serve_shares(int dtype, int64_t tokens, int64_t bytes) { return tokens > (dtype == SPARROW_F32 ? 32ll << 20 : 200ll << 20) / bytes; }
+// Over 8 bits the reads are cheaper and the keys not: what the rest costs goes by (token, KV head) rows.  Sharing begins at 1 Mi of them where requests have up
+// to 16 rows and tables for more than 1,536 tokens (fp32: 16 MiB), at 640 Ki beyond 32 rows.  us shared and not; up to 16 rows, heads of 64: 28 and 4 heads, 8 of
+// 25,500 (100 MiB, 0.8 Mi rows) 24.3 and 24.5, 64 of 3,100 27.1 and 24.8, 8 of 33,200 (130 MiB, 1.04 Mi) 26.8 and 30.5, 64 of 4,000 28.9 and 29.1; 32 and 8,
+// 24 of 5,400 (130 MiB) 23.1 and 29.6, 128 of 900 31.2 and 22.4; heads of 128, 64 of 2,900 (190 MiB, 0.76 Mi) 32.5 and 29.1.  56 rows, heads of 128, 17,000
+// tokens: 6 requests 46.7 and 39.6, 8 46.2 and 45.9, 10 (169 MiB, 676 Ki) 49.7 and 51.2, 11 49.7 and 59.2, 12 50.4 and 59.9; heads of 64, 32 of 5,000 (80 MiB)
+// 37.8 and 38.5, of 6,300 39.8 and 45.0.  17 to 32 rows, 32 and 8 heads of 64, 12 of 13,500 (160 MiB) 45.5 and 47.3, of 128, 32 of 3,000 (204 MiB) 44.6 and 42.2:
+// as bf16.  fp32, 28 and 4 heads of 128, 8 of 1,500 (12 MiB) 21.7 and 22.2, of 2,200 (18 MiB) 22.2 and 27.9; 6 of 2,900, 56 rows, 49.9 and 44.9.
+bool serve_shares(int dtype, bool eight, int d, int Hkv, int B, int64_t capacity, int64_t rows) {
+  const bool f32 = dtype == SPARROW_F32;
+  const int64_t tokens = B * capacity, bytes = 2ll * Hkv * d * (eight ? 1 : f32 ? 4 : 2), kv_rows = tokens * Hkv;
+  if (tokens > (f32 ? 32ll << 20 : 200ll << 20) / bytes) return true;
+  if (!eight) return false;
+  if (f32) return rows <= 16 && tokens > (16ll << 20) / bytes;
+  return rows > 32 ? kv_rows > 640 << 10 : rows <= 16 && capacity > 1536 && kv_rows > 1 << 20;
+}
 
 ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t n_rows, int max_new, int64_t capacity) {
   ServeShape s;

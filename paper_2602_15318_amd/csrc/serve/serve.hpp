@@ -56,8 +56,8 @@ struct ServeShape {
   int rows, waves, slots, round, ways, grid;
   int64_t floats_o, floats_ml;
 };
-// Whether prefixes are read once for their groups, by the tokens that the tables of the batch hold and the bytes of one token's keys and values.
-bool serve_shares(int dtype, int64_t tokens, int64_t bytes);
+// Whether prefixes are read once for their groups, by what the tables of the batch could hold: B of `capacity` tokens; rows: of a request, at most.
+bool serve_shares(int dtype, bool eight, int d, int Hkv, int B, int64_t capacity, int64_t rows);
 ServeShape serve_shape(int dtype, int d, int Hq, int Hkv, int B, int G, int64_t n_rows, int max_new, int64_t capacity);
 hipError_t launch_serve_attn(int dtype, int d, const ServeShape &s, const ServeArgs &a, hipStream_t st);
 

@@ -136,7 +136,7 @@ int attention(const sparrow_paged_desc *desc, const void *q, const void *k_cache
   a.scale_log2 = (desc->scale > 0.f ? desc->scale : 1.0f / std::sqrt((float)desc->head_dim)) * kLog2e;
   a.inv_g = 1.0f / (float)a.g;
   const int64_t capacity = (int64_t)table_width * desc->page_size;
-  a.G = serve_shares(desc->dtype, B * capacity, 2ll * a.Hkv * desc->head_dim * (exponents ? 1 : desc->dtype == SPARROW_F32 ? 4 : 2)) ? n_groups : 0;
+  a.G = serve_shares(desc->dtype, exponents != nullptr, desc->head_dim, a.Hkv, B, capacity, (int64_t)std::min(max_new, n_rows) * a.g) ? n_groups : 0;
   a.once = n_groups == 0 || a.G > 0;
   const ServeShape shape = serve_shape(desc->dtype, desc->head_dim, a.Hq, a.Hkv, B, a.G, n_rows, max_new, capacity);
   a.slots = shape.slots; a.round = shape.round; a.ways = shape.ways; a.block_shift = shift_of(shape.rows);
