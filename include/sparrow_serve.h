@@ -17,7 +17,7 @@
  * written, and a held element is a bf16 number that is read back without a rounding, or 2^128, which elements from 248 * 2^120 (3.3e38) on round to
  * and which is read back as infinite.
  * The strides of such a cache count bytes.  Contents are not trusted: a byte above 254 or below 1 is taken as the nearest of these, by the attention
- * one of V below 9 as 9.  Of powers that are not written, elements below 2^-133 are no bf16 numbers, and those from 2^128 on are infinite.
+ * one of V below 9 as 9.  Of powers that are not written, elements below 2^-133 are no bf16 numbers, and those from 2^128 on are infinite when read back.
  */
 #ifndef SPARROW_SERVE_H
 #define SPARROW_SERVE_H
@@ -81,6 +81,8 @@ int sparrow_chunk_attn8(const sparrow_paged_desc *desc, const void *q, const voi
  *  prefix_len   dev int32 [n_groups].  What is shared is cut to the tokens that come before the new ones of every request of the group (0 where
  *               one has no such tokens): the result does not change, the keys behind the cut are read request by request
  * Limits: as sparrow_chunk_attn, n_groups <= SPARROW_MAX_PREFIX_GROUPS.
+ * The workspace is asked for as for the widest tables, with the groups and without, whatever the call's tables hold; a piece's part of it is for a whole block
+ * of rows (16, 64 or 256).  28 and 4 heads of 128, a group of 32 single tokens: 136 MB, of 256 209 MB; 32 heads of each, 256 requests: 1.2 GB.
  */
 size_t sparrow_prefix_attn_workspace(const sparrow_paged_desc *desc, int32_t B, int32_t n_groups, int32_t n_rows, int32_t max_new);
 int sparrow_prefix_attn(const sparrow_paged_desc *desc, const void *q, const void *k_cache, const void *v_cache,

@@ -2,7 +2,9 @@
 // the group) of an item, products on the matrix cores in fp32.  As chunk_f32_kernel (../paged/chunk_attn_f32.hip): four wavefronts of 16 rows, K and
 // V tiles of 32 keys one tile ahead, two workgroups per compute unit.  An 8-bit cache's tiles come through registers and are written to LDS as the fp32
 // numbers that they are.
-// Bound by the fp32 matrix cores from some 64 rows on; five single tokens over 500 (a head of 64) 7 us, round trips.
+// Bound by the fp32 matrix cores from some 64 rows on: a chunk of 256 over 8,192, 28 and 4 heads of 128, 322 us.  Single tokens fill part of a wavefront's 16 rows and
+// leave three wavefronts idle: 48 over up to 8,192, 8 bits, 191 us, matrix cores busy for 45 and LDS for 60, a third of it bank conflicts of the tiles' writes and V's
+// reads.  Five over 500 (a head of 64) 7 us, round trips.
 #include "serve_tiles.hpp"
 
 namespace sparrow {

@@ -6,8 +6,10 @@
 // fill the time.  An 8-bit cache's have two, and their codes lie in LDS as they come; they become bf16 numbers in the operands, K's times its power, V's as they are, V's power in the probability.  A 16-byte read of K is a lane's part of two k-steps, Q^T cut alike; V^T of
 // eight keys is one transposing read of bytes (attn_few.hpp).
 //
-// Bound by memory and the round trips around it: twelve chains of 8 over up to 8,000, 28 and 4 heads of 128, 34.7 us with the second pass (in blocks of 256 rows
-// 44.4), one over 26,112 21.4 (24.7), with heads of 64 eight chains 27.0 (36.4), all 8 bits; in bf16 twelve chains over 8,300 35.0 (44.4).
+// Bound by waiting: a workgroup fills a compute unit's LDS, two wavefronts a SIMD.  Twelve chains of 8 over up to 8,000, 28 and 4 heads of 128, 8 bits, 35.4 us, 29 of
+// them here: the vector ALU works some 11 (of more than 32 rows, each half converts a tile for itself), the matrix cores 4, and 77 MB are fetched where 52 are
+// held.  Over bf16 pages, twice the bytes, 35.0.  In blocks of 256 rows 44.4 either way; one chain over 26,112 22.3 (24.7), with heads of 64 eight chains 27.7
+// (36.4).
 #pragma once
 #include "attn_few.hpp"
 
