@@ -8,7 +8,7 @@
 // Probabilities are rounded to bf16 for the output's product, half a step 2^-9 to 2^-8 of a term; the row's sum takes them unrounded.
 //
 // Bound by the matrix cores beside the exponentials: 2,048 tokens over 26,112, 28 and 4 heads of 128, 630 us in bf16 and 667 in 8 bits (1.17 and 1.10 PFLOP/s;
-// a product of 8,192^3 on that card 1.27; up to 650 and 688 on others), matrix cores busy 45 to 57 % of the cycles by the card's clock.  With heads of 64 a tile has the same softmax for half the
+// a product of 8,192^3 on that card 1.27; up to 650 and 716 on others), matrix cores busy 45 to 57 % of the cycles by the card's clock.  With heads of 64 a tile has the same softmax for half the
 // products.  A piece of a prefix (224 rows, 576 tokens) takes some 10 us beside its tiles: the first loads, and up to 128 KB of partial output.
 #pragma once
 #include "serve_tiles.hpp"
